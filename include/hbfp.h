@@ -70,7 +70,8 @@ typedef enum hbfp_status {
     HBFP_ERR_CUDA = 5,        /* a CUDA runtime/driver call failed (launch, tensor map, ...)  */
     HBFP_ERR_TIMEOUT = 6,     /* a bounded device-side wait expired (see hbfp_device_status) */
     HBFP_ERR_STATIC_LIMIT = 7, /* hbfp_gemm_static: the problem needs more than the built-in scratch */
-    HBFP_ERR_EXPONENT_RANGE = 8 /* hbfp_device_status: a tensor-core GEMM met block exponents outside its exact range */
+    HBFP_ERR_EXPONENT_RANGE = 8, /* hbfp_device_status: a tensor-core GEMM met block exponents outside its exact range */
+    HBFP_ERR_INDEX = 9        /* hbfp_device_status: a page number or a length in device memory was out of range */
 } hbfp_status;
 
 #define HBFP_ROUND_NEAREST_EVEN 0
@@ -381,6 +382,97 @@ HBFP_API int hbfp_gemm_block_partials(int64_t M, int64_t N, int64_t K, const hbf
                                       const hbfp_operand* b, int32_t* P, uint32_t impl,
                                       void* stream);
 
+/* ---- Serving operators ------------------------------------------------------------------
+ * What a trained network is served with beside hbfp_gemm_q: a product in 8-bit integers with a
+ * scale for each token and channel, and attention over a key/value cache held in 4-bit block
+ * floating point. Activations are FP32, bfloat16 or binary16, sums are int32 or FP32, the result
+ * has the activations' type. (The paper has no counterpart of the first; the cache is Eq. 1 with
+ * 4-bit mantissas, the narrowest of its design points, blocks of 32.) */
+#define HBFP_F32 0
+#define HBFP_BF16 1
+#define HBFP_F16 2
+#define HBFP_I8 3    /* hbfp_int8_gemm: activations that hbfp_int8_quantize has converted */
+
+/* Rows of 8-bit integers with one FP32 scale per row, the contraction along the row:
+ *   scale[r] = fl32(max_k |x[r][k]| / 127),   q[r][k] = x[r][k] / scale[r] rounded to the nearest
+ * whole number, halves to even, decided on the exact quotient (0 where the scale is 0).
+ * contract_axis 1: rows of x [d0][d1] (one scale per token); 0: its columns (one scale per output
+ * channel of weights stored [inputs][outputs]), q is then [d1][pitch] and scale [d1]. ld = elements
+ * between rows of x. pitch = bytes between rows of q: a multiple of 16, at least the contraction's
+ * length; bytes behind it up to the pitch are written as zeros. q must be 16-byte aligned. A row that holds
+ * an infinity or a NaN gets that as its scale (and yields infinities or NaN in products). */
+HBFP_API int hbfp_int8_quantize(const void* x, int dtype, int64_t d0, int64_t d1, int64_t ld, int contract_axis,
+                                int8_t* q, int64_t pitch, float* scale, void* stream);
+
+/* y [M][N] = sa[m] * sb[n] * sum_k a[m][k] * w[n][k] + bias[n], the sum exact in int32 (K < 131072).
+ * a: activations of type a_dtype, converted by the call as hbfp_int8_quantize does (a_scale null),
+ * or with a_dtype = HBFP_I8 rows that were converted before and their a_scale [M]; lda in elements
+ * (HBFP_I8: bytes, a multiple of 16, a 16-byte aligned). w [N][ldw] with w_scale [N]: rows per output
+ * channel, ldw a multiple of 16, w 16-byte aligned. bias: FP32 [N] or null. y of type y_dtype (not
+ * HBFP_I8), ldy in elements. The workspace (256-byte aligned, hbfp_int8_gemm_workspace bytes, host-only
+ * query) holds converted activations where the product's kernel does not convert them itself. */
+HBFP_API int hbfp_int8_gemm_workspace(int64_t M, int64_t N, int64_t K, int a_dtype, size_t* bytes);
+HBFP_API int hbfp_int8_gemm(int64_t M, int64_t N, int64_t K, const void* a, int a_dtype, int64_t lda, const float* a_scale,
+                            const int8_t* w, int64_t ldw, const float* w_scale, const float* bias, void* y, int y_dtype,
+                            int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Paged key/value cache in 4-bit block floating point. A page holds `page` tokens (a power of two, 16
+ * or more) of every head; a row of `dim` values (64, 96, 128 or 256) is dim/32 blocks of 32 with one
+ * exponent s in [-63, 120]: value = q * 2^s, |q| <= 7, stored as nibble q + 8. Every 32-bit word holds
+ * eight consecutive values, value 2i in nibble i and value 2i+1 in nibble i+4. Arrays:
+ *   mantissas uint8 [pages][heads][page][dim/2], exponents int8 [pages][heads][page][dim/32],
+ * 16-byte aligned, one pair for keys and one for values. Set struct_size = sizeof(hbfp_kv4_cache). */
+typedef struct hbfp_kv4_cache {
+    uint32_t struct_size;
+    int32_t heads, dim, page;
+    int64_t pages;
+    uint8_t* k_mant;
+    int8_t* k_exps;
+    uint8_t* v_mant;
+    int8_t* v_exps;
+} hbfp_kv4_cache;
+
+/* The tokens of a call. Sequence b has length[b] tokens in the cache once the call's own are in it (device
+ * int32); position p of it lies in page table[b*table_ld + p/page], row p % page (device int32, table_pages
+ * entries of a row are valid memory; entries behind the sequence's last page are not looked at). The
+ * call's tokens are rows of q, k, v and the output: sequence b owns rows [starts[b], starts[b+1]) (device
+ * int32 [sequences+1], at most max_tokens each), or with starts null max_tokens = tokens / sequences rows
+ * each. Row i of n of a sequence stands at position length - n + i; a row whose position is negative is
+ * not written to the cache and sees no key. Rows behind the last sequence's are left as they are. A length
+ * of 0 or less is an empty sequence. Set struct_size. */
+typedef struct hbfp_kv4_batch {
+    uint32_t struct_size;
+    int32_t sequences;
+    const int32_t* table;
+    int64_t table_ld;
+    int32_t table_pages;
+    int32_t max_tokens;
+    const int32_t* lengths;
+    const int32_t* starts; /* may be null */
+    int64_t tokens;
+} hbfp_kv4_batch;
+
+/* Writes the call's keys and values [tokens][heads][dim] (element strides of a token and a head, dim
+ * contiguous) into the cache, converted with nearest-even rounding; values beyond 7 * 2^120 saturate.
+ * Mantissas and exponents are those of hbfp_quantize with mant_bits 4 and block 32. The positions written must be
+ * distinct rows of the cache: sequences may share pages that they only read. Inputs must be finite. */
+HBFP_API int hbfp_kv4_append(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int dtype, const void* k, int64_t k_token,
+                             int64_t k_head, const void* v, int64_t v_token, int64_t v_head, void* stream);
+
+/* FP32 values of the last `count` positions of every sequence, k and v [sequences*count][heads][dim], zeros where
+ * a position is negative (batch: table and lengths only). */
+HBFP_API int hbfp_kv4_read(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int32_t count, float* k, float* v, void* stream);
+
+/* out[row][head] = sum_j p_j v_j with p = softmax_j(scale * q[row][head] . k_j) over the positions j <= own position
+ * (and > own position - window where window > 0) of the row's sequence. q and out [tokens][heads*group][dim] (element strides,
+ * dim contiguous); query head i reads KV head i / group. A row that sees no key is zeros. Append the call's own keys first. The
+ * workspace (256-byte aligned) takes the parts of a sequence that several CTAs share. */
+HBFP_API int hbfp_kv4_attention_workspace(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int dtype, int32_t group,
+                                          int32_t window, size_t* bytes);
+HBFP_API int hbfp_kv4_attention(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int dtype, const void* q, int64_t q_token,
+                                int64_t q_head, int32_t group, float scale, int32_t window, void* out, int64_t out_token, int64_t out_head,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
 /* Host-only: kind of GEMM kernel that the calling thread's most recent hbfp_gemm, hbfp_gemm_q, hbfp_gemm_q_bias,
  * hbfp_gemm_static or hbfp_gemm_block_partials call launched: "gemm_tc2_kernel" (two SMs per 256 x 256 tile),
  * "gemm_tc_kernel" (the other tensor-core products, the floating-point operand forms among them), "gemm_skinny_kernel" (a few
@@ -405,7 +497,9 @@ HBFP_API int hbfp_last_gemm_cycles(uint64_t* cycles);
  * device in *status (host int): 0, or a code recorded by a kernel. Codes below 900: a bounded wait
  * on a barrier expired (the kernel then abandons its work and exits; HBFP_ERR_TIMEOUT is returned).
  * Codes 900-999: a tensor-core GEMM met block exponents outside the range in which its scaled
- * accumulation is exact (see hbfp_gemm; HBFP_ERR_EXPONENT_RANGE is returned). */
+ * accumulation is exact (see hbfp_gemm; HBFP_ERR_EXPONENT_RANGE is returned). Codes from 1000: a
+ * hbfp_kv4_* kernel met a page number outside the cache (1001) or a length beyond the page table
+ * or token ranges out of order (1002), and left those keys or tokens out (HBFP_ERR_INDEX is returned). */
 HBFP_API int hbfp_device_status(void* stream, int32_t* status);
 
 /* Self-test of the bounded waits (the paper has no counterpart: failure behaviour of this

@@ -19,7 +19,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("HBFP_LIBRARY") or os.path.join(_HERE, "libhbfp.so")
 
 (OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT,
- ERR_STATIC_LIMIT, ERR_EXPONENT_RANGE) = range(9)
+ ERR_STATIC_LIMIT, ERR_EXPONENT_RANGE, ERR_INDEX) = range(10)
 STATIC_WORKSPACE_BYTES = 16 << 20
 GEMM_AUTO, GEMM_FORCE_SIMT, GEMM_FORCE_TENSOR, GEMM_FORCE_TENSOR_1SM, GEMM_FORCE_TENSOR_2SM, GEMM_FORCE_SMALL = 0, 1, 2, 3, 4, 5
 ROUND_NEAREST_EVEN, ROUND_STOCHASTIC = 0, 1
@@ -30,6 +30,7 @@ EXPORTS = [
     "hbfp_gemm_q_workspace", "hbfp_gemm", "hbfp_gemm_q", "hbfp_gemm_q_bias", "hbfp_column_sums", "hbfp_fold_taps", "hbfp_gemm_block_partials",
     "hbfp_device_status", "hbfp_gemm_static", "hbfp_wide_quantize", "hbfp_wide_update", "hbfp_wide_update_value", "hbfp_wide_narrow",
     "hbfp_im2col_packed", "hbfp_im2col_packed_t", "hbfp_wide_dequantize", "hbfp_selftest_bounded_wait", "hbfp_last_gemm_kernel", "hbfp_last_gemm_launch", "hbfp_last_gemm_cycles", "hbfp_conv_forward", "hbfp_quantize_conv_weights", "hbfp_conv_dgrad_filters",
+    "hbfp_int8_quantize", "hbfp_int8_gemm_workspace", "hbfp_int8_gemm", "hbfp_kv4_append", "hbfp_kv4_read", "hbfp_kv4_attention_workspace", "hbfp_kv4_attention",
 ]
 
 
@@ -116,6 +117,14 @@ def lib() -> ctypes.CDLL:
         L.hbfp_selftest_bounded_wait.argtypes = [i64, i32, p, p]
         L.hbfp_last_gemm_cycles.argtypes = [p]
         L.hbfp_fold_taps.argtypes = [p, i64, i64, i64, i64, i32, i32, i32, p, p]
+        f32 = ctypes.c_float
+        L.hbfp_int8_quantize.argtypes = [p, i32, i64, i64, i64, i32, p, i64, p, p]
+        L.hbfp_int8_gemm_workspace.argtypes = [i64, i64, i64, i32, p]
+        L.hbfp_int8_gemm.argtypes = [i64, i64, i64, p, i32, i64, p, p, i64, p, p, p, i32, i64, p, sz, p]
+        L.hbfp_kv4_append.argtypes = [p, p, i32, p, i64, i64, p, i64, i64, p]
+        L.hbfp_kv4_read.argtypes = [p, p, i32, p, p, p]
+        L.hbfp_kv4_attention_workspace.argtypes = [p, p, i32, i32, i32, p]
+        L.hbfp_kv4_attention.argtypes = [p, p, i32, p, i64, i64, i32, f32, i32, p, i64, i64, p, sz, p]
         for fn in (L.hbfp_last_gemm_kernel, L.hbfp_last_gemm_launch):
             fn.restype = ctypes.c_char_p
             fn.argtypes = []
@@ -129,7 +138,8 @@ def lib() -> ctypes.CDLL:
 # Entry points that _host calls, in the order it takes them (csrc/host.cpp, struct Api).
 _HOST_ENTRY_POINTS = ("hbfp_packed_layout", "hbfp_quantize", "hbfp_gemm_q_workspace", "hbfp_wide_update_value", "hbfp_wide_dequantize",
                       "hbfp_conv_forward", "hbfp_conv_dgrad_filters", "hbfp_im2col_packed_t", "hbfp_im2col_packed", "hbfp_gemm_q_bias",
-                      "hbfp_column_sums", "hbfp_fold_taps")
+                      "hbfp_column_sums", "hbfp_fold_taps", "hbfp_int8_quantize", "hbfp_int8_gemm_workspace", "hbfp_int8_gemm",
+                      "hbfp_kv4_append", "hbfp_kv4_read", "hbfp_kv4_attention_workspace", "hbfp_kv4_attention")
 
 
 def host():
@@ -466,6 +476,96 @@ def gemm_block_partials(a: Packed, b: Packed, impl: int = GEMM_FORCE_SIMT) -> to
     return P
 
 
+# ------------------------------------------------------------------------------ serving operators
+
+_DTYPE_CODES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+@dataclass
+class Int8Rows:
+    """Rows of 8-bit integers with one FP32 scale each (see ``hbfp_int8_quantize``): tokens, or a layer's output channels."""
+    q: torch.Tensor        # int8 [rows][pitch], pitch a multiple of 16
+    scale: torch.Tensor    # float32 [rows]
+    k: int                 # length of the contraction
+
+    def dequantize(self) -> torch.Tensor:
+        """The FP32 values [rows][k]."""
+        return self.q[:, :self.k].float() * self.scale[:, None]
+
+
+def int8_quantize(x: torch.Tensor, contract_axis: int = 1, out: Optional[Int8Rows] = None) -> Int8Rows:
+    """hbfp_int8_quantize: the rows of the 2-D float32, bfloat16 or float16 CUDA tensor ``x`` (``contract_axis`` 1, one scale
+    per token) or its columns (0, one scale per output channel of weights ``[inputs][outputs]``)."""
+    k = x.shape[contract_axis] if x.dim() == 2 and contract_axis in (0, 1) else 0
+    if out is not None and out.k != k:
+        raise ValueError("out has another contraction length")
+    q, s = _got((_native or host()).int8_quantize(x, contract_axis, out.q if out is not None else None, out.scale if out is not None else None),
+                "hbfp_int8_quantize")
+    return out if out is not None else Int8Rows(q, s, k)
+
+
+def int8_gemm(x, w: Int8Rows, bias: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+              dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """hbfp_int8_gemm: ``x [M][K]`` (a tensor, converted token by token by the call, or ``Int8Rows``) times the output channels
+    ``w`` (rows = outputs), plus ``bias`` (float32 ``[N]``). The result ``[M][N]`` has x's type unless ``dtype`` or ``out`` says
+    otherwise (float32 for ``Int8Rows``)."""
+    if isinstance(x, Int8Rows):
+        if x.k != w.k:
+            raise ValueError("contraction extents differ")
+        xq, xs = x.q, x.scale
+    else:
+        xq, xs = x, None
+    if dtype is not None and (dtype not in _DTYPE_CODES or out is not None and out.dtype != dtype):
+        raise ValueError("dtype must be float32, bfloat16 or float16, and out's where there is one")
+    return _got((_native or host()).int8_gemm(xq, xs, w.k, w.q, w.scale, bias, out, -1 if dtype is None else _DTYPE_CODES[dtype]), "hbfp_int8_gemm")
+
+
+@dataclass
+class Kv4Cache:
+    """A paged key/value cache in 4-bit block floating point (``hbfp_kv4_cache``): uint8 mantissas
+    ``[pages][heads][page][dim / 2]`` and int8 exponents ``[pages][heads][page][dim / 32]``, for keys and for values."""
+    k_mant: torch.Tensor
+    k_exps: torch.Tensor
+    v_mant: torch.Tensor
+    v_exps: torch.Tensor
+
+
+def kv4_alloc(pages: int, heads: int, page: int, dim: int, device="cuda") -> Kv4Cache:
+    """An empty cache: ``pages`` pages of ``page`` tokens (a power of two, 16 or more) of ``heads`` KV heads of ``dim`` values
+    (64, 96, 128 or 256). Nothing reads a row that was not appended, so it is not cleared."""
+    if page < 16 or page & (page - 1) or dim not in (64, 96, 128, 256) or pages < 0 or heads < 1:
+        raise ValueError("page must be a power of two, 16 or more, dim one of 64, 96, 128 and 256")
+    m = [torch.empty((pages, heads, page, dim // 2), dtype=torch.uint8, device=device) for _ in range(2)]
+    e = [torch.empty((pages, heads, page, dim // 32), dtype=torch.int8, device=device) for _ in range(2)]
+    return Kv4Cache(m[0], e[0], m[1], e[1])
+
+
+def kv4_append(cache: Kv4Cache, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+               starts: Optional[torch.Tensor] = None, max_tokens: Optional[int] = None) -> None:
+    """hbfp_kv4_append: new tokens' keys and values ``[tokens][heads][dim]`` (any strides of tokens and heads) into the cache.
+    ``page_table`` int32 ``[sequences][pages]``; ``lengths`` int32 ``[sequences]``: tokens of each sequence, these included.
+    Without ``starts`` every sequence has the same number of rows; with it (int32 ``[sequences + 1]``) sequence b owns rows
+    ``starts[b]`` to ``starts[b + 1]``, at most ``max_tokens`` (host number; all rows where it is not given)."""
+    _check((_native or host()).kv4_append(cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps, page_table, lengths, k, v, starts, max_tokens),
+           "hbfp_kv4_append")
+
+
+def kv4_read(cache: Kv4Cache, count: int, page_table: torch.Tensor, lengths: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """hbfp_kv4_read: the FP32 keys and values ``[sequences * count][heads][dim]`` of the last ``count`` positions of every sequence
+    (zeros where there is no position)."""
+    return _got((_native or host()).kv4_read(cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps, page_table, lengths, count), "hbfp_kv4_read")
+
+
+def kv4_attention(q: torch.Tensor, cache: Kv4Cache, page_table: torch.Tensor, lengths: torch.Tensor, scale: Optional[float] = None,
+                  window: int = 0, starts: Optional[torch.Tensor] = None, max_tokens: Optional[int] = None,
+                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """hbfp_kv4_attention: causal attention of ``q [tokens][heads * group][dim]`` (any strides of tokens and heads) over the cache,
+    the last ``window`` positions of it where that is not 0; ``scale`` is 1 / sqrt(dim) unless given. Tokens, ``page_table``, ``lengths``, ``starts`` and
+    ``max_tokens`` as in ``kv4_append``, which writes the call's own keys and values first. A row that sees no key is zeros."""
+    return _got((_native or host()).kv4_attention(cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps, page_table, lengths, q, scale, window, starts,
+                                                  max_tokens, out), "hbfp_kv4_attention")
+
+
 def last_gemm_cycles() -> int:
     """hbfp_last_gemm_cycles: SM cycles of the longest CTA of the most recent paired-SM GEMM launch (synchronises)."""
     out = ctypes.c_uint64(0)
@@ -489,8 +589,8 @@ def device_status() -> int:
 
 
 def device_status_rc():
-    """hbfp_device_status as (return code, recorded code): (OK, 0), (ERR_TIMEOUT, code below 900) or
-    (ERR_EXPONENT_RANGE, code 900-999)."""
+    """hbfp_device_status as (return code, recorded code): (OK, 0), (ERR_TIMEOUT, code below 900),
+    (ERR_EXPONENT_RANGE, code 900-999) or (ERR_INDEX, code from 1000)."""
     v = ctypes.c_int32()
     rc = lib().hbfp_device_status(_stream(), ctypes.byref(v))
     return rc, v.value

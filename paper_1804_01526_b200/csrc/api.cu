@@ -61,7 +61,7 @@ int read_clear_device_status(cudaStream_t st, int32_t* out) {
     HBFP_CUDA_OK(cudaMemcpyToSymbol(g_device_status, &zero, sizeof(zero)));
     *out = v;
     if (v == 0) return HBFP_OK;
-    return v >= 900 && v < 1000 ? HBFP_ERR_EXPONENT_RANGE : HBFP_ERR_TIMEOUT;
+    return v >= 1000 ? HBFP_ERR_INDEX : v >= 900 ? HBFP_ERR_EXPONENT_RANGE : HBFP_ERR_TIMEOUT;
 }
 
 namespace {
@@ -339,6 +339,7 @@ const char* hbfp_status_string(int status) {
         case HBFP_ERR_TIMEOUT: return "bounded device-side wait expired";
         case HBFP_ERR_EXPONENT_RANGE: return "operand exponents outside the tensor-core path's exact range";
         case HBFP_ERR_STATIC_LIMIT: return "problem exceeds the built-in scratch of hbfp_gemm_static";
+        case HBFP_ERR_INDEX: return "page number or length in device memory out of range";
         default: return "unknown status";
     }
 }

@@ -15,6 +15,7 @@
 #include <ATen/core/LegacyTypeDispatch.h>
 #include <ATen/cuda/CUDAContext.h>
 #include <c10/cuda/CUDACachingAllocator.h>
+#include <c10/cuda/CUDAGuard.h>
 
 #include "hbfp.h"
 
@@ -35,6 +36,13 @@ struct Api {
     decltype(&hbfp_gemm_q_bias) gemm_q_bias;
     decltype(&hbfp_column_sums) column_sums;
     decltype(&hbfp_fold_taps) fold_taps;
+    decltype(&hbfp_int8_quantize) int8_quantize;
+    decltype(&hbfp_int8_gemm_workspace) int8_gemm_workspace;
+    decltype(&hbfp_int8_gemm) int8_gemm;
+    decltype(&hbfp_kv4_append) kv4_append;
+    decltype(&hbfp_kv4_read) kv4_read;
+    decltype(&hbfp_kv4_attention_workspace) kv4_attention_workspace;
+    decltype(&hbfp_kv4_attention) kv4_attention;
 } api;
 
 // ------------------------------------------------------------------------------ arguments
@@ -699,6 +707,263 @@ PyObject* conv3x3(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ------------------------------------------------------------------------------ serving operators
+
+// The calls below run on the device of their first tensor, whichever is current, and on that device's current stream.
+
+int dtype_of(const at::Tensor& x) {
+    switch (x.scalar_type()) {
+        case at::kFloat: return HBFP_F32;
+        case at::kBFloat16: return HBFP_BF16;
+        case at::kHalf: return HBFP_F16;
+        default: return -1;
+    }
+}
+void require(bool ok, const char* what) {
+    if (ok) return;
+    PyErr_SetString(PyExc_ValueError, what);
+    throw Fail{};
+}
+void check_device(const at::Tensor& x, const at::Tensor& first, const char* name) {
+    if (!(x.is_cuda() && x.device() == first.device())) value_error("%s must be a CUDA tensor on the device of the others", name);
+}
+c10::DataPtr scratch(size_t bytes) {
+    return bytes ? c10::cuda::CUDACachingAllocator::get()->allocate(bytes) : c10::DataPtr();
+}
+
+// int8_quantize(x, axis, q or None, scale or None) -> (q, scale)
+PyObject* int8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!want(n, 4)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const at::Tensor x = tensor_of(a[0], "x");
+        const int dt = dtype_of(x);
+        require(x.is_cuda() && dt >= 0 && x.dim() == 2 && (x.size(1) <= 1 || x.stride(1) == 1) && (x.size(0) <= 1 || x.stride(0) >= x.size(1)),
+                "x must be a 2-D float32, bfloat16 or float16 CUDA tensor with contiguous rows");
+        const int axis = (int)as_ll(a[1]);
+        require(axis == 0 || axis == 1, "contract_axis is 0 or 1");
+        const int64_t rows = x.size(axis == 1 ? 0 : 1), k = x.size(axis == 1 ? 1 : 0);
+        const bool fresh = a[2] == Py_None;
+        at::Tensor q, s;
+        if (!fresh) {
+            q = tensor_of(a[2], "q");
+            s = tensor_of(a[3], "scale");
+            check_device(q, x, "q");
+            check_device(s, x, "scale");
+            require(q.scalar_type() == at::kChar && q.dim() == 2 && q.size(0) == rows && q.size(1) >= k && q.is_contiguous(), "q must be a contiguous int8 tensor [rows][pitch]");
+            require(s.scalar_type() == at::kFloat && s.dim() == 1 && s.size(0) == rows && s.is_contiguous(), "scale must be a contiguous float32 tensor [rows]");
+        }
+        const int rc = without_gil([&] {
+            const c10::cuda::CUDAGuard guard(x.device());
+            if (fresh) {
+                q = at::empty({rows, std::max<int64_t>((k + 15) / 16 * 16, 16)}, x.options().dtype(at::kChar).requires_grad(false));
+                s = empty_f32({rows}, x);
+            }
+            return api.int8_quantize(x.data_ptr(), dt, x.size(0), x.size(1), ld_of(x), axis, (int8_t*)q.data_ptr(), q.size(1), (float*)s.data_ptr(), cur_stream());
+        });
+        if (rc) return code(rc);
+        return Py_BuildValue("(NN)", fresh ? THPVariable_Wrap(q) : same(a[2]), fresh ? THPVariable_Wrap(s) : same(a[3]));
+    });
+}
+
+// int8_gemm(x, x_scale or None, k, w, w_scale, bias or None, out or None, dtype of the result as in hbfp.h, -1: x's) -> out
+PyObject* int8_gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!want(n, 8)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        const at::Tensor x = tensor_of(a[0], "x"), w = tensor_of(a[3], "w"), ws = tensor_of(a[4], "w.scale");
+        const bool converted = a[1] != Py_None, fresh = a[6] == Py_None;
+        const int64_t K = as_ll(a[2]), M = x.dim() == 2 ? x.size(0) : 0, N = w.dim() == 2 ? w.size(0) : 0;
+        int dt = converted ? HBFP_I8 : dtype_of(x), odt = (int)as_ll(a[7]);
+        at::Tensor xs, bias, out;
+        require(x.is_cuda() && x.dim() == 2 && (x.size(1) <= 1 || x.stride(1) == 1) && (x.size(0) <= 1 || x.stride(0) >= x.size(1)), "x must be a 2-D CUDA tensor with contiguous rows");
+        if (converted) {
+            xs = tensor_of(a[1], "x.scale");
+            check_device(xs, x, "x.scale");
+            require(x.scalar_type() == at::kChar && x.size(1) >= K, "x.q must be an int8 tensor [rows][pitch]");
+            require(xs.scalar_type() == at::kFloat && xs.dim() == 1 && xs.size(0) == M && xs.is_contiguous(), "x.scale must be a contiguous float32 tensor [rows]");
+        } else {
+            require(dt >= 0, "x must be float32, bfloat16 or float16, or Int8Rows");
+            require(x.size(1) == K, "contraction extents differ");
+        }
+        check_device(w, x, "w");
+        check_device(ws, x, "w.scale");
+        require(w.scalar_type() == at::kChar && w.dim() == 2 && w.size(1) >= K && (w.size(1) <= 1 || w.stride(1) == 1) && (N <= 1 || w.stride(0) >= w.size(1)),
+                "w.q must be an int8 tensor [rows][pitch]");
+        require(ws.scalar_type() == at::kFloat && ws.dim() == 1 && ws.size(0) == N && ws.is_contiguous(), "w.scale must be a contiguous float32 tensor [rows]");
+        if (a[5] != Py_None) {
+            bias = tensor_of(a[5], "bias");
+            check_device(bias, x, "bias");
+            require(bias.scalar_type() == at::kFloat && bias.dim() == 1 && bias.size(0) == N && bias.is_contiguous(), "bias must be a contiguous float32 tensor [outputs]");
+        }
+        if (!fresh) {
+            out = tensor_of(a[6], "out");
+            check_device(out, x, "out");
+            require(dtype_of(out) >= 0 && out.dim() == 2 && out.size(0) == M && out.size(1) == N && (N <= 1 || out.stride(1) == 1) && (M <= 1 || out.stride(0) >= N),
+                    "out must be a float32, bfloat16 or float16 tensor [rows of x][outputs] with contiguous rows");
+            odt = dtype_of(out);
+        } else if (odt < 0) {
+            odt = converted ? HBFP_F32 : dt;
+        }
+        const int rc = without_gil([&] {
+            const c10::cuda::CUDAGuard guard(x.device());
+            if (fresh) out = at::empty({M, N}, x.options().dtype(odt == HBFP_F32 ? at::kFloat : odt == HBFP_BF16 ? at::kBFloat16 : at::kHalf).requires_grad(false));
+            size_t bytes = 0;
+            const int bad = api.int8_gemm_workspace(M, N, K, dt, &bytes);
+            if (bad) return bad;
+            const c10::DataPtr mem = scratch(bytes);
+            return api.int8_gemm(M, N, K, x.data_ptr(), dt, ld_of(x), converted ? (const float*)xs.data_ptr() : nullptr, (const int8_t*)w.data_ptr(), ld_of(w), (const float*)ws.data_ptr(),
+                                 bias.defined() ? (const float*)bias.data_ptr() : nullptr, out.data_ptr(), odt, ld_of(out), mem.get(), bytes, cur_stream());
+        });
+        if (rc) return code(rc);
+        return fresh ? THPVariable_Wrap(out) : same(a[6]);
+    });
+}
+
+// A cache (k_mant, k_exps, v_mant, v_exps in order) and a call's tokens (table, lengths, starts or None, most tokens of a sequence, tokens).
+struct Kv4Call {
+    at::Tensor arrays[4], table, lengths, starts;
+    hbfp_kv4_cache cache{};
+    hbfp_kv4_batch batch{};
+    Kv4Call(PyObject* const* a) {
+        for (int i = 0; i < 4; ++i) {
+            arrays[i] = tensor_of(a[i], "cache");
+            check_device(arrays[i], arrays[0], "cache");
+            require(arrays[i].dim() == 4 && arrays[i].is_contiguous() && arrays[i].scalar_type() == (i & 1 ? at::kChar : at::kByte),
+                    "the cache is contiguous uint8 mantissas [pages][heads][page][dim / 2] and int8 exponents [pages][heads][page][dim / 32]");
+            for (int d = 0; d < 3; ++d) require(arrays[i].size(d) == arrays[0].size(d), "the cache's arrays differ in pages, heads or page length");
+            require(arrays[i].size(3) * (i & 1 ? 16 : 1) == arrays[0].size(3), "the cache's arrays differ in width");
+        }
+        const at::Tensor& m = arrays[0];
+        require(m.size(1) < (1 << 30) && m.size(2) < (1 << 30) && m.size(3) < (1 << 28), "the cache's extents are out of range");
+        cache.struct_size = sizeof(cache);
+        cache.pages = m.size(0);
+        cache.heads = (int32_t)m.size(1);
+        cache.page = (int32_t)m.size(2);
+        cache.dim = (int32_t)m.size(3) * 2;
+        cache.k_mant = (uint8_t*)m.data_ptr();
+        cache.k_exps = (int8_t*)arrays[1].data_ptr();
+        cache.v_mant = (uint8_t*)arrays[2].data_ptr();
+        cache.v_exps = (int8_t*)arrays[3].data_ptr();
+        table = tensor_of(a[4], "page_table");
+        lengths = tensor_of(a[5], "lengths");
+        check_device(table, m, "page_table");
+        check_device(lengths, m, "lengths");
+        require(table.scalar_type() == at::kInt && table.dim() == 2 && (table.size(1) <= 1 || table.stride(1) == 1) && table.stride(0) >= 0, "page_table must be an int32 tensor [sequences][pages]");
+        require(lengths.scalar_type() == at::kInt && lengths.dim() == 1 && lengths.is_contiguous() && lengths.size(0) == table.size(0), "lengths must be a contiguous int32 tensor [sequences]");
+        require(table.size(0) < (1 << 30) && table.size(1) < (1 << 30), "page_table is too large");
+        batch.struct_size = sizeof(batch);
+        batch.sequences = (int32_t)table.size(0);
+        batch.table = (const int32_t*)table.data_ptr();
+        batch.table_pages = (int32_t)table.size(1);
+        batch.table_ld = table.size(0) > 1 ? table.stride(0) : table.size(1);
+        batch.lengths = (const int32_t*)lengths.data_ptr();
+    }
+    // The call's tokens: rows of a tensor of so many.
+    void tokens(int64_t rows, PyObject* st, PyObject* most) {
+        batch.tokens = rows;
+        if (st == Py_None) {
+            require(most == Py_None, "max_tokens goes with starts");
+            require(batch.sequences > 0 ? rows % batch.sequences == 0 : rows == 0, "without starts every sequence has the same number of tokens");
+            const int64_t each = batch.sequences > 0 ? rows / batch.sequences : 0;
+            require(each < (1 << 30), "too many tokens");
+            batch.max_tokens = (int32_t)each;
+            return;
+        }
+        starts = tensor_of(st, "starts");
+        check_device(starts, arrays[0], "starts");
+        require(starts.scalar_type() == at::kInt && starts.dim() == 1 && starts.is_contiguous() && starts.size(0) == (int64_t)batch.sequences + 1,
+                "starts must be a contiguous int32 tensor [sequences + 1]");
+        const int64_t m = most == Py_None ? rows : as_ll(most);
+        require(m >= 0 && m < (1 << 30), "max_tokens is out of range");
+        batch.starts = (const int32_t*)starts.data_ptr();
+        batch.max_tokens = (int32_t)std::min<int64_t>(m, rows);
+    }
+    // A [tokens][heads][dim] tensor of the call.
+    void check_rows(const at::Tensor& x, int64_t heads, const char* name) const {
+        check_device(x, arrays[0], name);
+        if (!(dtype_of(x) >= 0 && x.dim() == 3 && x.size(1) == heads && x.size(2) == cache.dim && x.stride(2) == 1 && x.stride(0) >= 0 && x.stride(1) >= 0))
+            value_error("%s must be a float32, bfloat16 or float16 tensor [tokens][heads][dim] with contiguous rows", name);
+    }
+};
+
+// kv4_append(4 arrays, table, lengths, k, v, starts or None, max_tokens or None)
+PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!want(n, 10)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        Kv4Call c(a);
+        const at::Tensor k = tensor_of(a[6], "k"), v = tensor_of(a[7], "v");
+        c.check_rows(k, c.cache.heads, "k");
+        c.check_rows(v, c.cache.heads, "v");
+        require(k.scalar_type() == v.scalar_type() && k.size(0) == v.size(0), "k and v differ in type or tokens");
+        c.tokens(k.size(0), a[8], a[9]);
+        const int rc = without_gil([&] {
+            const c10::cuda::CUDAGuard guard(k.device());
+            return api.kv4_append(&c.cache, &c.batch, dtype_of(k), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), cur_stream());
+        });
+        return code(rc);
+    });
+}
+
+// kv4_read(4 arrays, table, lengths, count) -> (k, v)
+PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!want(n, 7)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        Kv4Call c(a);
+        const int64_t count = as_ll(a[6]);
+        require(count >= 0 && count < (1 << 30), "count is out of range");
+        at::Tensor k, v;
+        const int rc = without_gil([&] {
+            const c10::cuda::CUDAGuard guard(c.table.device());
+            const auto o = c.table.options().dtype(at::kFloat);
+            k = at::empty({c.batch.sequences * count, c.cache.heads, c.cache.dim}, o);
+            v = at::empty({c.batch.sequences * count, c.cache.heads, c.cache.dim}, o);
+            return api.kv4_read(&c.cache, &c.batch, (int32_t)count, (float*)k.data_ptr(), (float*)v.data_ptr(), cur_stream());
+        });
+        if (rc) return code(rc);
+        return Py_BuildValue("(NN)", THPVariable_Wrap(k), THPVariable_Wrap(v));
+    });
+}
+
+// kv4_attention(4 arrays, table, lengths, q, scale or None, window, starts or None, max_tokens or None, out or None) -> out
+PyObject* kv4_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!want(n, 12)) return nullptr;
+    return guarded([&]() -> PyObject* {
+        Kv4Call c(a);
+        const at::Tensor q = tensor_of(a[6], "q");
+        const int64_t heads = q.dim() == 3 ? q.size(1) : 0;
+        c.check_rows(q, heads, "q");
+        require(heads > 0 && heads % c.cache.heads == 0, "the query heads must be a multiple of the cache's heads");
+        require(heads < (1 << 30), "too many heads");
+        double scale = 1.0 / std::sqrt((double)std::max(c.cache.dim, 1));
+        if (a[7] != Py_None) {
+            scale = PyFloat_AsDouble(a[7]);
+            if (scale == -1.0 && PyErr_Occurred()) throw Fail{};
+        }
+        const int64_t window = as_ll(a[8]);
+        require(window >= 0, "window is 0 (none) or the number of positions that a row sees");
+        c.tokens(q.size(0), a[9], a[10]);
+        const bool fresh = a[11] == Py_None;
+        at::Tensor out;
+        if (!fresh) {
+            out = tensor_of(a[11], "out");
+            c.check_rows(out, heads, "out");
+            require(out.scalar_type() == q.scalar_type() && out.size(0) == q.size(0), "out must have the type and the rows of q");
+        }
+        const int rc = without_gil([&] {
+            const c10::cuda::CUDAGuard guard(q.device());
+            if (fresh) out = at::empty(q.sizes(), q.options().requires_grad(false));
+            const int group = (int)(heads / c.cache.heads), w = (int)std::min<int64_t>(window, 1 << 30);
+            size_t bytes = 0;
+            const int bad = api.kv4_attention_workspace(&c.cache, &c.batch, dtype_of(q), group, w, &bytes);
+            if (bad) return bad;
+            const c10::DataPtr mem = scratch(bytes);
+            return api.kv4_attention(&c.cache, &c.batch, dtype_of(q), q.data_ptr(), q.stride(0), q.stride(1), group, (float)scale, w, out.data_ptr(), out.stride(0), out.stride(1),
+                                     mem.get(), bytes, cur_stream());
+        });
+        if (rc) return code(rc);
+        return fresh ? THPVariable_Wrap(out) : same(a[11]);
+    });
+}
+
 // bind(type of the error to raise, addresses in the order of Api)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     constexpr Py_ssize_t N = sizeof(Api) / sizeof(void*);
@@ -722,7 +987,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define HBFP_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HBFP_METHOD(bind), HBFP_METHOD(packed_layout), HBFP_METHOD(quantize), HBFP_METHOD(gemm), HBFP_METHOD(gemm_q), HBFP_METHOD(wide_update),
                          HBFP_METHOD(wide_dequantize), HBFP_METHOD(conv_forward), HBFP_METHOD(conv_dgrad_filters),
-                         HBFP_METHOD(im2col_packed_t), HBFP_METHOD(linear), HBFP_METHOD(conv3x3),
+                         HBFP_METHOD(im2col_packed_t), HBFP_METHOD(linear), HBFP_METHOD(conv3x3), HBFP_METHOD(int8_quantize), HBFP_METHOD(int8_gemm),
+                         HBFP_METHOD(kv4_append), HBFP_METHOD(kv4_read), HBFP_METHOD(kv4_attention),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

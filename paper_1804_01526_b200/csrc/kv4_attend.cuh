@@ -1,0 +1,630 @@
+// Attention of a few query rows over the 4-bit cache, with warp-level bfloat16 MMAs.
+//
+// For one sequence and one KV head the rows are the call's queries times the query heads that share the head. Scores are computed
+// transposed, S^T = K Q^T (16 keys x 8 rows an MMA), and so is the result, O^T = V^T P^T: both wide operands come from the cache, a
+// lane's share of a key or value row is a run of words that it loads with one instruction and unpacks in registers, and eight rows
+// fill the narrow side, where the usual order would pad a single token's rows to sixteen. The order of the 16 values along an MMA's
+// contraction is free as long as both operands agree, so the unpacked pairs need no shuffling; scores become the second product's
+// operand by one 8 x 8 transpose (movmatrix).
+//
+// A cached value, nibble * 2^s, is a bfloat16 exactly: (128 + nibble) is put together with one logical instruction and
+// fma(128 + nibble, 2^s, -136 * 2^s) rounds nothing. Queries and probabilities are split into as many bfloat16 parts as their type
+// has bits (1 for bfloat16, 2 for binary16, 3 for FP32: of a query nothing is left, of a probability 2^-8, 2^-16, 2^-24), so
+// products are exact and sums FP32. Softmax in base 2, running maximum and sum in FP32.
+//
+// Bound: reading the cache, dim / 2 + dim / 32 bytes per key and head and as much for values. Warps take 32 keys each in turn (16 of a
+// 256-wide head) and keep their own maximum and sum; the CTA joins them once at the end of its keys.
+//
+// Split. Sequences differ in length and the host does not know the lengths, so a launch with long keys has as many CTAs as the GPU
+// holds at a time and each takes an equal share of all units (128 keys of one sequence, head and row tile), found by adding up the
+// lengths itself. A tile whose keys end up in several CTAs leaves FP32 parts (at most two a CTA) that a second launch joins in
+// ascending order: the same result every time.
+#pragma once
+
+#include <atomic>
+
+#include "kv4.cuh"
+#include "tc_ptx.cuh"
+
+namespace hbfp {
+
+struct Kv4Attend {
+    Kv4Args c;
+    const void* q;
+    Kv4Rows qs;
+    void* out;
+    Kv4Rows os;
+    int group;              // query heads of a KV head
+    int window;             // 0: none
+    float scale2;           // scale * log2(e)
+    int tiles;              // row tiles of a sequence at most
+    float* partial;         // split launches: [2 * CTAs][rows of a tile][dim], then [2 * CTAs][rows][2] (maximum, sum)
+    int ctas;
+};
+
+int launch_kv4_attend_f32(const Kv4Attend& a, cudaStream_t st, size_t* bytes);
+int launch_kv4_attend_bf16(const Kv4Attend& a, cudaStream_t st, size_t* bytes);
+int launch_kv4_attend_f16(const Kv4Attend& a, cudaStream_t st, size_t* bytes);
+
+namespace {
+
+constexpr int KA_WARPS = 4, KA_THREADS = 32 * KA_WARPS;
+
+template <int D> struct KaDim {
+    static constexpr int NB = D / 32;                      // blocks of a row; words of a key row that a lane takes
+    static constexpr int VW = (D + 63) / 64;               // words of a value row that a lane takes (96: as 128, the last lanes none)
+    static constexpr int CH = D <= 128 ? 32 : 16;          // keys of a warp at a time
+    static constexpr int UNIT = CH * KA_WARPS;             // keys of a CTA at a time
+    static constexpr int STEPS = D / 16;                   // MMA steps along a key row
+    static constexpr int KE = D == 128 || D == 64 ? 1 : 2; // exponents of a lane's key words
+};
+template <int D, int NP, int NT> struct KaShared {                      // queries, then the warps' results in their place; maxima and sums
+    static constexpr int Q = NP * NT * KaDim<D>::STEPS * 256, OP = D + 4, O = KA_WARPS * 8 * NT * OP * 4;
+    static constexpr int ML = Q > O ? Q : O, BYTES = ML + KA_WARPS * 8 * NT * 8;
+};
+
+__device__ __forceinline__ void ka_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint2 b) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b.x), "r"(b.y));
+}
+__device__ __forceinline__ uint32_t ka_transpose(uint32_t v) {
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
+}
+// 2^s of two neighbours as a pair of bfloat16, and -136 * 2^s
+__device__ __forceinline__ uint32_t ka_scale(int s0, int s1) { return (uint32_t)((s0 + 127) | ((s1 + 127) << 16)) << 7; }
+__device__ __forceinline__ uint32_t ka_offset(uint32_t scale) {
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(scale), "r"(0xC308C308u));
+    return d;
+}
+// The pair of values whose nibbles are the low four bits of w's halfwords.
+__device__ __forceinline__ uint32_t ka_value(uint32_t w, uint32_t scale, uint32_t offset) {
+    uint32_t d, n;
+    asm("lop3.b32 %0, %1, 0x000F000F, 0x43004300, 0xEA;" : "=r"(n) : "r"(w));
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(n), "r"(scale), "r"(offset));
+    return d;
+}
+// The parts of two FP32 values as pairs of bfloat16: the first the values rounded, each later one what is left.
+template <int NP>
+__device__ __forceinline__ void ka_parts(float a, float b, uint32_t (&d)[NP]) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        d[i] = pack_pair(a, b, (const __nv_bfloat16*)nullptr);
+        a -= __uint_as_float(d[i] << 16);
+        b -= __uint_as_float(d[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ float ka_exp2(float x) {
+    float d;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(x));
+    return d;
+}
+
+template <int N>
+__device__ __forceinline__ void ka_load_words(const uint32_t* p, uint32_t (&w)[N]) {
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(p + i));
+            w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+        }
+    } else if constexpr (N == 2) {
+        const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+        w[0] = v.x; w[1] = v.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = __ldg(p + i);
+    }
+}
+
+// The keys [lo, hi) that the rows of a tile see, lo rounded down to a whole group of sixteen.
+struct KaRange { int lo, hi; };
+
+// Row tile `tile` of (sequence b, head h): keys [lo, hi), result into `out` (slot < 0) or as a part.
+template <int D, int NP, int NT, class T>
+__device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq& seq, int h, int tile, KaRange range, int slot, unsigned char* sm) {
+    using C = KaDim<D>;
+    constexpr int RT = 8 * NT, MT = C::CH / 16, TILES = 4 * C::VW;        // TILES: 16-row tiles of V^T
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int rows = min(RT, seq.n * a.group - tile * RT), r0 = tile * RT;
+    uint2* qs = reinterpret_cast<uint2*>(sm);                             // [NP][NT][STEPS][32]
+    __syncthreads();                                                      // the tile before is through with shared memory
+    for (int i = threadIdx.x; i < NT * C::STEPS * 32; i += KA_THREADS) {
+        const int l = i & 31, step = (i >> 5) % C::STEPS, nt = (i >> 5) / C::STEPS, r = 8 * nt + (l >> 2);
+        float e[4] = {0.f, 0.f, 0.f, 0.f};
+        if (r < rows) {
+            const int query = (r0 + r) / a.group, gh = (r0 + r) - query * a.group;
+            const T* src = reinterpret_cast<const T*>(a.q) + (seq.first + query) * a.qs.token + (h * a.group + gh) * a.qs.head + ((l & 3) * C::NB + (step >> 1)) * 8 + 4 * (step & 1);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = to_f32(src[j]);
+        }
+        uint32_t x[NP], y[NP];
+        ka_parts<NP>(e[0], e[1], x);
+        ka_parts<NP>(e[2], e[3], y);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) qs[p * (NT * C::STEPS * 32) + i] = make_uint2(x[p], y[p]);
+    }
+    // positions of this lane's rows (columns 2 t and 2 t + 1 of every eight): keys up to there are seen
+    int limit[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) limit[nt][c] = seq.length - seq.n + (r0 + min(8 * nt + 2 * t + c, rows - 1)) / a.group;
+    const int first_limit = seq.length - seq.n + r0 / a.group, last_limit = seq.length - seq.n + (r0 + rows - 1) / a.group;
+    const int window = a.window ? a.window : 0x7fffffff;
+    __syncthreads();
+
+    float o[TILES][NT][4], m[NT][2], l[NT][2];
+#pragma unroll
+    for (int i = 0; i < TILES; ++i)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][nt][e] = 0.f;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) { m[nt][c] = -INFINITY; l[nt][c] = 0.f; }
+
+    uint32_t kw[MT][2][C::NB], vw[MT][4][C::VW];
+    int8_t ke[MT][2][C::KE], ve[MT][4];
+    const int ke0 = (t * C::NB) >> 2;
+    // row of the cache's arrays where the sixteen keys from p on begin; -1: none of them are there
+    auto group_row = [&](int p) -> int64_t {
+        if (p >= range.hi) return -1;
+        const int64_t page = kv4_page(a.c, b, p >> a.c.shift);
+        return page < 0 ? -1 : ((page * a.c.heads + h) << a.c.shift) + (p & (a.c.page - 1));
+    };
+    auto load_keys = [&](const int64_t (&row)[MT]) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) {
+                const int64_t at = max(row[i], (int64_t)0) + g + 8 * hh;
+                if (row[i] >= 0) {
+                    ka_load_words<C::NB>(reinterpret_cast<const uint32_t*>(a.c.k_mant) + at * (D / 8) + t * C::NB, kw[i][hh]);
+#pragma unroll
+                    for (int e = 0; e < C::KE; ++e) ke[i][hh][e] = __ldg(a.c.k_exps + at * C::NB + min(ke0 + e, C::NB - 1));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < C::NB; ++e) kw[i][hh][e] = 0;
+#pragma unroll
+                    for (int e = 0; e < C::KE; ++e) ke[i][hh][e] = 0;
+                }
+            }
+    };
+    auto load_values = [&](const int64_t (&row)[MT]) {
+        const int ve0 = (g * C::VW) >> 2;
+        const bool mine = D % 64 == 0 || g * C::VW < D / 8;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t at = max(row[i], (int64_t)0) + 2 * t + (j & 1) + 8 * (j >> 1);
+                if (row[i] >= 0 && mine) {
+                    ka_load_words<C::VW>(reinterpret_cast<const uint32_t*>(a.c.v_mant) + at * (D / 8) + g * C::VW, vw[i][j]);
+                    ve[i][j] = __ldg(a.c.v_exps + at * C::NB + ve0);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < C::VW; ++e) vw[i][j][e] = 0;
+                    ve[i][j] = 0;
+                }
+            }
+    };
+
+    int64_t row[MT];
+    int pos = range.lo + warp * C::CH;
+    if (pos < range.hi) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) row[i] = group_row(pos + 16 * i);
+        load_keys(row);
+        load_values(row);
+    }
+    for (; pos < range.hi; pos += C::UNIT) {
+        // ---- S^T = K Q^T
+        float s[MT][NT][4];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[i][nt][e] = 0.f;
+        uint32_t sc[MT][2][C::KE], of[MT][2][C::KE];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+                for (int e = 0; e < C::KE; ++e) {
+                    const int x = kv4_exponent(ke[i][hh][e]);
+                    sc[i][hh][e] = ka_scale(x, x);
+                    of[i][hh][e] = ka_offset(sc[i][hh][e]);
+                }
+#pragma unroll
+        for (int j = 0; j < C::NB; ++j) {
+            // which of the lane's exponents: all words in one block, or (256) four in each, or (96) split by lane
+            uint32_t scj[MT][2], ofj[MT][2];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh) {
+                    const bool second = C::KE == 2 && ((t * C::NB + j) >> 2) != ke0;
+                    scj[i][hh] = second ? sc[i][hh][C::KE - 1] : sc[i][hh][0];
+                    ofj[i][hh] = second ? of[i][hh][C::KE - 1] : of[i][hh][0];
+                }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                uint32_t f[MT][4];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    f[i][0] = ka_value(kw[i][0][j] >> (8 * u), scj[i][0], ofj[i][0]);
+                    f[i][1] = ka_value(kw[i][1][j] >> (8 * u), scj[i][1], ofj[i][1]);
+                    f[i][2] = ka_value(kw[i][0][j] >> (8 * u + 4), scj[i][0], ofj[i][0]);
+                    f[i][3] = ka_value(kw[i][1][j] >> (8 * u + 4), scj[i][1], ofj[i][1]);
+                }
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const uint2 q = qs[((p * NT + nt) * C::STEPS + 2 * j + u) * 32 + lane];
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) ka_mma(s[i][nt], f[i][0], f[i][1], f[i][2], f[i][3], q);
+                    }
+            }
+        }
+        bool whole = pos + C::CH <= range.hi && pos + C::CH - 1 <= first_limit && last_limit - pos < window;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) whole = whole && row[i] >= 0;
+        int64_t next[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) next[i] = group_row(pos + C::UNIT + 16 * i);
+        load_keys(next);
+
+        // ---- softmax in base 2: this lane holds keys g and g + 8 of every sixteen for its rows
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[i][nt][e] *= a.scale2;
+                    if (!whole) {
+                        const int p = pos + 16 * i + g + 8 * (e >> 1);
+                        if (row[i] < 0 || p >= range.hi || p > limit[nt][e & 1] || limit[nt][e & 1] - p >= window) s[i][nt][e] = -INFINITY;
+                    }
+                }
+        float top[NT][2];
+        bool grows = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float x = fmaxf(s[0][nt][c], s[0][nt][c + 2]);
+#pragma unroll
+                for (int i = 1; i < MT; ++i) x = fmaxf(x, fmaxf(s[i][nt][c], s[i][nt][c + 2]));
+                top[nt][c] = x;
+                grows |= x > m[nt][c];
+            }
+        if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float x = fmaxf(m[nt][c], top[nt][c]);
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+                    const float f = x == -INFINITY ? 0.f : ka_exp2(m[nt][c] - x);
+                    m[nt][c] = x;
+                    l[nt][c] *= f;
+#pragma unroll
+                    for (int i = 0; i < TILES; ++i) { o[i][nt][c] *= f; o[i][nt][c + 2] *= f; }
+                }
+        }
+        uint2 pb[MT][NT][NP];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const float p0 = ka_exp2(s[i][nt][0] - m0), p1 = ka_exp2(s[i][nt][1] - m1), p2 = ka_exp2(s[i][nt][2] - m0), p3 = ka_exp2(s[i][nt][3] - m1);
+                l[nt][0] += p0 + p2;
+                l[nt][1] += p1 + p3;
+                uint32_t x[NP], y[NP];
+                ka_parts<NP>(p0, p1, x);
+                ka_parts<NP>(p2, p3, y);
+#pragma unroll
+                for (int p = 0; p < NP; ++p) pb[i][nt][p] = make_uint2(ka_transpose(x[p]), ka_transpose(y[p]));
+            }
+        }
+        // ---- O^T += V^T P^T
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const uint32_t s01 = ka_scale(kv4_exponent(ve[i][0]), kv4_exponent(ve[i][1])), s23 = ka_scale(kv4_exponent(ve[i][2]), kv4_exponent(ve[i][3]));
+            const uint32_t o01 = ka_offset(s01), o23 = ka_offset(s23);
+#pragma unroll
+            for (int w = 0; w < C::VW; ++w) {
+                const uint32_t x01 = __byte_perm(vw[i][0][w], vw[i][1][w], 0x5410), y01 = __byte_perm(vw[i][0][w], vw[i][1][w], 0x7632);
+                const uint32_t x23 = __byte_perm(vw[i][2][w], vw[i][3][w], 0x5410), y23 = __byte_perm(vw[i][2][w], vw[i][3][w], 0x7632);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t f0 = ka_value(x01 >> (4 * e), s01, o01), f1 = ka_value(y01 >> (4 * e), s01, o01);
+                    const uint32_t f2 = ka_value(x23 >> (4 * e), s23, o23), f3 = ka_value(y23 >> (4 * e), s23, o23);
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) ka_mma(o[4 * w + e][nt], f0, f1, f2, f3, pb[i][nt][p]);
+                }
+            }
+        }
+        load_values(next);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) row[i] = next[i];
+    }
+
+    // ---- the warps' parts joined
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], d);
+    __syncthreads();                                                      // all are through with the queries
+    constexpr int OP = KaShared<D, NP, NT>::OP;
+    float* os = reinterpret_cast<float*>(sm);                             // [KA_WARPS][RT][OP]
+    float2* ml = reinterpret_cast<float2*>(sm + KaShared<D, NP, NT>::ML);      // [KA_WARPS][RT]
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            const int d = (C::VW * g + (i >> 2)) * 8 + 2 * (i & 3);
+            if (D % 64 == 0 || d < D) {
+                float* at = os + (warp * RT + 8 * nt + 2 * t) * OP + d;
+                *reinterpret_cast<float2*>(at) = make_float2(o[i][nt][0], o[i][nt][2]);
+                *reinterpret_cast<float2*>(at + OP) = make_float2(o[i][nt][1], o[i][nt][3]);
+            }
+        }
+        if (g == 0)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) ml[warp * RT + 8 * nt + 2 * t + c] = make_float2(m[nt][c], l[nt][c]);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * (D / 4); i += KA_THREADS) {
+        const int r = i / (D / 4), d = 4 * (i - r * (D / 4));
+        float top = -INFINITY, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < KA_WARPS; ++w) top = fmaxf(top, ml[w * RT + r].x);
+        if (top != -INFINITY)
+#pragma unroll
+            for (int w = 0; w < KA_WARPS; ++w) {
+                const float2 x = ml[w * RT + r];
+                const float f = ka_exp2(x.x - top);
+                const float4 y = *reinterpret_cast<const float4*>(os + (w * RT + r) * OP + d);
+                sum += f * x.y;
+                v[0] += f * y.x; v[1] += f * y.y; v[2] += f * y.z; v[3] += f * y.w;
+            }
+        if (slot >= 0) {
+            float* part = a.partial + ((int64_t)slot * RT + r) * D + d;
+            *reinterpret_cast<float4*>(part) = make_float4(v[0], v[1], v[2], v[3]);
+            if (d == 0) reinterpret_cast<float2*>(a.partial + (int64_t)2 * a.ctas * RT * D)[(int64_t)slot * RT + r] = make_float2(top, sum);
+            continue;
+        }
+        const float inv = sum > 0.f ? __frcp_rn(sum) : 0.f;               // a row that sees no key: zeros
+        const int query = (r0 + r) / a.group, gh = (r0 + r) - query * a.group;
+        T* dst = reinterpret_cast<T*>(a.out) + (seq.first + query) * a.os.token + (h * a.group + gh) * a.os.head + d;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dst[e] = from_f32<T>(v[e] * inv);
+    }
+}
+
+__device__ __forceinline__ KaRange ka_range(const Kv4Attend& a, const Kv4Seq& s, int first_query, int last_query) {
+    KaRange r;
+    const int base = s.length - s.n;
+    r.hi = max(0, min(s.length, base + last_query + 1));
+    r.lo = a.window ? max(0, base + first_query - a.window + 1) & ~15 : 0;
+    return r;
+}
+
+// A tile per CTA: short keys, or tiles enough.
+template <int D, int NP, int NT, class T>
+__global__ void __launch_bounds__(KA_THREADS)
+kv4_attend_kernel(const Kv4Attend a) {
+    extern __shared__ __align__(16) unsigned char sm[];
+    chain_start();
+    const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x;
+    const Kv4Seq s = kv4_seq(a.c, b);
+    constexpr int RT = 8 * NT;
+    if (tile * RT >= s.n * a.group) return;
+    const int last = min((tile + 1) * RT, s.n * a.group) - 1;
+    ka_tile<D, NP, NT, T>(a, b, s, h, tile, ka_range(a, s, tile * RT / a.group, last / a.group), -1, sm);
+}
+
+// The units of a sequence's tiles (all alike) and how many tiles it has.
+template <int D, int NT>
+__device__ __forceinline__ int2 ka_units(const Kv4Attend& a, const Kv4Seq& s) {
+    const KaRange r = ka_range(a, s, 0, s.n - 1);
+    const int tiles = (s.n * a.group + 8 * NT - 1) / (8 * NT) * a.c.heads;
+    return make_int2(max(1, (r.hi - r.lo + KaDim<D>::UNIT - 1) / KaDim<D>::UNIT), tiles);
+}
+// Units of all sequences and of those before each thread's share of them, by all threads of the CTA.
+template <int D, int NT>
+__device__ __forceinline__ void ka_scan(const Kv4Attend& a, int& total, int& before, int& b0, int& b1) {
+    __shared__ int sums[KA_WARPS];
+    const int per = (a.c.sequences + KA_THREADS - 1) / KA_THREADS;
+    b0 = min(a.c.sequences, (int)threadIdx.x * per);
+    b1 = min(a.c.sequences, b0 + per);
+    int own = 0;
+    for (int b = b0; b < b1; ++b) {
+        const int2 u = ka_units<D, NT>(a, kv4_seq(a.c, b));
+        own += u.x * u.y;
+    }
+    int x = own;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, d);
+        if ((threadIdx.x & 31) >= d) x += y;
+    }
+    if ((threadIdx.x & 31) == 31) sums[threadIdx.x >> 5] = x;
+    __syncthreads();
+    total = 0;
+    before = x - own;
+#pragma unroll
+    for (int w = 0; w < KA_WARPS; ++w) {
+        if (w < (int)(threadIdx.x >> 5)) before += sums[w];
+        total += sums[w];
+    }
+}
+
+template <int D, int NP, int NT, class T>
+__global__ void __launch_bounds__(KA_THREADS)
+kv4_attend_split_kernel(const Kv4Attend a) {
+    extern __shared__ __align__(16) unsigned char sm[];
+    __shared__ int found[2];
+    chain_start();
+    int total, before, b0, b1;
+    ka_scan<D, NT>(a, total, before, b0, b1);
+    const int ctas = min(a.ctas, total), cta = blockIdx.x;
+    if (cta >= ctas) return;
+    int u = (int)((int64_t)total * cta / ctas);
+    const int end = (int)((int64_t)total * (cta + 1) / ctas);
+    for (int b = b0; b < b1; ++b) {
+        const int2 x = ka_units<D, NT>(a, kv4_seq(a.c, b));
+        if (u >= before && u < before + x.x * x.y) { found[0] = b; found[1] = u - before; }
+        before += x.x * x.y;
+    }
+    __syncthreads();
+    int b = found[0], at = found[1];
+    while (u < end && b < a.c.sequences) {
+        const Kv4Seq s = kv4_seq(a.c, b);
+        const int2 x = ka_units<D, NT>(a, s);
+        const KaRange all = ka_range(a, s, 0, s.n - 1);
+        while (u < end && at < x.x * x.y) {
+            const int item = at / x.x, within = at - item * x.x, take = min(x.x - within, end - u);
+            const int tile = item / a.c.heads, h = item - tile * a.c.heads;
+            KaRange r;
+            r.lo = all.lo + within * KaDim<D>::UNIT;
+            r.hi = min(all.hi, r.lo + take * KaDim<D>::UNIT);
+            const int slot = take == x.x ? -1 : 2 * cta + (within == 0);
+            ka_tile<D, NP, NT, T>(a, b, s, h, tile, r, slot, sm);
+            at += take;
+            u += take;
+        }
+        ++b;
+        at = 0;
+    }
+}
+
+// The parts of the tiles that were split, joined in ascending order of their keys. A CTA per tile.
+template <int D, int NT, class T>
+__global__ void __launch_bounds__(KA_THREADS)
+kv4_join_kernel(const Kv4Attend a) {
+    constexpr int RT = 8 * NT;
+    __shared__ int found[2];
+    chain_start();
+    const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x;
+    int total, before, b0, b1;
+    ka_scan<D, NT>(a, total, before, b0, b1);
+    const Kv4Seq s = kv4_seq(a.c, b);
+    const int2 x = ka_units<D, NT>(a, s);
+    const int item = tile * a.c.heads + h;
+    if (item >= x.y) return;
+    if (b >= b0 && b < b1) {
+        for (int c = b0; c < b; ++c) {
+            const int2 y = ka_units<D, NT>(a, kv4_seq(a.c, c));
+            before += y.x * y.y;
+        }
+        found[0] = before;
+    }
+    __syncthreads();
+    const int64_t ctas = min(a.ctas, total);
+    const int first = found[0] + item * x.x;
+    const int c0 = (int)(((int64_t)(first + 1) * ctas - 1) / total), c1 = (int)(((int64_t)(first + x.x) * ctas - 1) / total);
+    if (c0 == c1) return;
+    const int rows = min(RT, s.n * a.group - tile * RT);
+    const float2* ml = reinterpret_cast<const float2*>(a.partial + (int64_t)2 * a.ctas * RT * D);
+    for (int i = threadIdx.x; i < rows * (D / 4); i += KA_THREADS) {
+        const int r = i / (D / 4), d = 4 * (i - r * (D / 4));
+        float top = -INFINITY, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int c = c0; c <= c1; ++c) top = fmaxf(top, ml[(int64_t)(2 * c + (c == c0)) * RT + r].x);
+        if (top != -INFINITY)
+            for (int c = c0; c <= c1; ++c) {
+                const int64_t at = (int64_t)(2 * c + (c == c0)) * RT + r;
+                const float2 y = ml[at];
+                const float f = ka_exp2(y.x - top);
+                const float4 w = *reinterpret_cast<const float4*>(a.partial + at * D + d);
+                sum += f * y.y;
+                v[0] += f * w.x; v[1] += f * w.y; v[2] += f * w.z; v[3] += f * w.w;
+            }
+        const float inv = sum > 0.f ? __frcp_rn(sum) : 0.f;
+        const int query = (tile * RT + r) / a.group, gh = tile * RT + r - query * a.group;
+        T* dst = reinterpret_cast<T*>(a.out) + (s.first + query) * a.os.token + (h * a.group + gh) * a.os.head + d;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dst[e] = from_f32<T>(v[e] * inv);
+    }
+}
+
+// ------------------------------------------------------------------------------ host side
+
+// With `bytes` the workspace is asked for and nothing is launched.
+template <int D, int NP, int NT, class T>
+int ka_launch(Kv4Attend a, cudaStream_t st, size_t* bytes) {
+    constexpr int SMEM = KaShared<D, NP, NT>::BYTES;
+    static std::atomic<int> resident[MAX_DEVICES];
+    const int dev = current_device();
+    if (dev < 0) return HBFP_ERR_CUDA;
+    int ctas = resident[dev].load(std::memory_order_acquire);
+    if (!ctas) {
+        int rc = allow_shared<kv4_attend_kernel<D, NP, NT, T>>(SMEM);
+        if (!rc) rc = allow_shared<kv4_attend_split_kernel<D, NP, NT, T>>(SMEM);
+        if (rc) return rc;
+        int per = 0;
+        HBFP_CUDA_OK(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kv4_attend_split_kernel<D, NP, NT, T>, KA_THREADS, SMEM));
+        if (per < 1) return HBFP_ERR_CUDA;
+        ctas = per * sm_count();
+        resident[dev].store(ctas, std::memory_order_release);
+    }
+    constexpr int RT = 8 * NT;
+    const int64_t cap = (int64_t)a.c.table_pages << a.c.shift;
+    const int64_t keys = a.window && (int64_t)a.window + a.c.most + 15 < cap ? (int64_t)a.window + a.c.most + 15 : cap;
+    a.tiles = (int)(((int64_t)a.c.most * a.group + RT - 1) / RT);
+    const int64_t items = (int64_t)a.tiles * a.c.heads * a.c.sequences, units = (keys + KaDim<D>::UNIT - 1) / KaDim<D>::UNIT;
+    const dim3 grid((unsigned)a.tiles, (unsigned)a.c.heads, (unsigned)a.c.sequences);
+    // A launch more and the parts' way through memory pay where a tile is long and the tiles do not fill the GPU several times.
+    const bool split = units > 2 && items < 4 * (int64_t)ctas && items * units < (1ll << 30);
+    if (bytes) {
+        *bytes = split ? (size_t)2 * ctas * RT * (D + 2) * sizeof(float) : 0;
+        return HBFP_OK;
+    }
+    if (!split) {
+        launch_chained(kv4_attend_kernel<D, NP, NT, T>, grid, KA_THREADS, SMEM, st, a);
+        return launch_status();
+    }
+    a.ctas = ctas;
+    launch_chained(kv4_attend_split_kernel<D, NP, NT, T>, dim3((unsigned)ctas), KA_THREADS, SMEM, st, a);
+    launch_chained(kv4_join_kernel<D, NT, T>, grid, KA_THREADS, 0, st, a);
+    return launch_status();
+}
+
+// Row tiles of 8, 16 or 32 (a 256-wide head: 16, its accumulators take twice the registers).
+template <int D, int NP, class T>
+int ka_launch_rows(const Kv4Attend& a, cudaStream_t st, size_t* bytes) {
+    const int64_t rows = (int64_t)a.c.most * a.group;
+    if (rows <= 8) return ka_launch<D, NP, 1, T>(a, st, bytes);
+    if constexpr (D <= 128)
+        if (rows > 16) return ka_launch<D, NP, 4, T>(a, st, bytes);
+    return ka_launch<D, NP, 2, T>(a, st, bytes);
+}
+template <int NP, class T>
+int ka_launch_dim(const Kv4Attend& a, cudaStream_t st, size_t* bytes) {
+    switch (a.c.dim) {
+        case 64: return ka_launch_rows<64, NP, T>(a, st, bytes);
+        case 96: return ka_launch_rows<96, NP, T>(a, st, bytes);
+        case 128: return ka_launch_rows<128, NP, T>(a, st, bytes);
+        case 256: return ka_launch_rows<256, NP, T>(a, st, bytes);
+    }
+    return HBFP_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+}  // namespace hbfp

@@ -1,0 +1,39 @@
+"""A trained dense layer for serving: its product in 8-bit integers with a scale for each token and channel.
+
+Training keeps the weights in block floating point (``HbfpLinear``); a network that is only run is served with one integer
+product per layer (``hbfp_int8_gemm``): the weights are converted once, one FP32 scale per output channel, the activations by
+every call, one scale per token. Between such layers attention reads a cache held in 4-bit block floating point
+(``binding.kv4_append``, ``binding.kv4_attention``), whose calls take the layers' outputs as they are, slices of a fused projection
+among them.
+"""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+
+from . import binding as hb
+from .autograd import HbfpLinear
+
+
+class Int8Linear(torch.nn.Module):
+    """``y = x W + b`` for inference, W ``[fin][fout]`` held as 8-bit integers; no gradients."""
+
+    def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor] = None):
+        """``weight`` [fin][fout]: float32, bfloat16 or float16 on the GPU, converted here; ``bias`` [fout], kept as float32."""
+        super().__init__()
+        self.fin, self.fout = weight.shape
+        rows = hb.int8_quantize(weight.detach(), 0)
+        self.register_buffer("weight_q", rows.q)
+        self.register_buffer("weight_scale", rows.scale)
+        self.register_buffer("bias", None if bias is None else bias.detach().float().contiguous())
+
+    @classmethod
+    def from_hbfp(cls, layer: HbfpLinear) -> "Int8Linear":
+        """The layer with the value of a trained ``HbfpLinear``'s weights."""
+        return cls(layer.weight, layer.bias)
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        """x [..][fin] float32, bfloat16 or float16; the result has its type. Leading extents that are one run of rows are taken as they are."""
+        y = hb.int8_gemm(x.detach().reshape(-1, self.fin), hb.Int8Rows(self.weight_q, self.weight_scale, self.fin), bias=self.bias)
+        return y.view(*x.shape[:-1], self.fout)

@@ -1,0 +1,610 @@
+"""Serving operators on the GPU against the definitions in 64 bits: the 8-bit integer product with a scale for each token and
+channel, the 4-bit cache and attention over it.
+
+Tolerances are bounds, derived beside each: u(t) = finfo(t).eps / 2 is the half step of a type."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def u(t):
+    return torch.finfo(t).eps / 2
+
+
+@pytest.fixture(scope="module")
+def hb():
+    from paper_1804_01526_b200 import binding
+    yield binding
+    assert binding.device_status() == 0
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def normal(g, *shape):
+    return torch.randn(shape, generator=g, device="cuda")
+
+
+# ----------------------------------------------------------------------------- 8-bit integers
+
+
+def int8_reference(x):
+    """(q, scale) of rows, in 64 bits on the host."""
+    x = x.double().cpu().numpy()
+    top = np.abs(x).max(axis=1, initial=0)
+    s = (top / 127).astype(np.float32)
+    q = np.where(s[:, None] > 0, np.rint(x / np.where(s > 0, s, 1).astype(np.float64)[:, None]), 0)
+    return np.clip(q, -127, 127).astype(np.int8), s
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,k", [(1, 1), (3, 7), (5, 16), (2, 129), (33, 1000), (4, 2049), (2, 9001), (1, 70000)])
+def test_int8_quantize_rows(hb, dtype, rows, k):
+    x = normal(gen(rows + k), rows, k).mul_(3).to(dtype)
+    x[0, k // 2] = 0
+    r = hb.int8_quantize(x)
+    q, s = int8_reference(x)
+    assert r.q.shape == (rows, max(16, -(-k // 16) * 16)) and r.k == k
+    assert np.array_equal(r.scale.cpu().numpy(), s)
+    assert np.array_equal(r.q[:, :k].cpu().numpy(), q)
+    assert not r.q[:, k:].any()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("k,cols", [(1, 1), (7, 3), (128, 32), (129, 33), (1000, 65), (300, 200)])
+def test_int8_quantize_columns_are_the_rows_of_the_transpose(hb, dtype, k, cols):
+    x = normal(gen(k + cols), k, cols + 3).to(dtype)[:, 1:cols + 1]           # rows further apart than they are long, and unaligned
+    r, t = hb.int8_quantize(x, 0), hb.int8_quantize(x.t().contiguous(), 1)
+    assert torch.equal(r.q, t.q) and torch.equal(r.scale, t.scale) and r.k == k
+    q, s = int8_reference(x.t())
+    assert np.array_equal(r.q[:, :k].cpu().numpy(), q)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_int8_quantize_ties_zero_rows_and_scales_at_the_ends(hb, dtype):
+    half = torch.arange(-127, 127, device="cuda").float() + 0.5
+    rows = [torch.cat([torch.tensor([127.0], device="cuda"), half]),                                   # scale 1: every value a tie, to even
+            torch.zeros(255, device="cuda"),
+            torch.cat([torch.tensor([127.0 * 2.0 ** -20], device="cuda"), half * 2.0 ** -20]),
+            torch.cat([torch.tensor([3.0], device="cuda"), torch.linspace(-3, 3, 254, device="cuda")])]
+    if dtype == torch.float32:
+        rows.append(torch.linspace(-1.0e-41, 1.0e-41, 255, device="cuda"))                             # a scale that is no normal number
+        rows.append(torch.linspace(-1.0, 1.0, 255, device="cuda") * 3.0e38)
+        rows.append(torch.linspace(-2.0e-44, 2.0e-44, 255, device="cuda"))                             # the scale rounds to zero
+    x = torch.stack(rows).to(dtype)
+    r = hb.int8_quantize(x)
+    q, s = int8_reference(x)
+    assert np.array_equal(r.scale.cpu().numpy(), s) and np.array_equal(r.q[:, :255].cpu().numpy(), q)
+    assert torch.equal(r.q[0, 1:255].int() % 2, torch.zeros(254, dtype=torch.int32, device="cuda"))
+
+
+def test_int8_quantize_views_and_out(hb):
+    x = normal(gen(1), 40, 530).bfloat16()
+    for v in (x[:, :512], x[:, 1:514], x[::3, 5:6], x[7:8]):
+        q, s = int8_reference(v)
+        r = hb.int8_quantize(v)
+        assert np.array_equal(r.q[:, :v.shape[1]].cpu().numpy(), q) and np.array_equal(r.scale.cpu().numpy(), s)
+    out = hb.Int8Rows(torch.full((40, 544), 77, dtype=torch.int8, device="cuda"), torch.empty(40, device="cuda"), 530)
+    assert hb.int8_quantize(x, out=out) is out
+    assert not out.q[:, 530:].any() and np.array_equal(out.q[:, :530].cpu().numpy(), int8_reference(x)[0])
+    assert torch.equal(out.dequantize(), out.q[:, :530].float() * out.scale[:, None])
+    empty = hb.int8_quantize(x[:0])
+    assert empty.q.shape == (0, 544) and empty.scale.shape == (0,)
+
+
+def test_int8_rows_with_infinities_and_nan_stay_by_themselves(hb):
+    x = normal(gen(2), 4, 64)
+    x[1, 3], x[2, 5] = math.inf, math.nan
+    w = hb.int8_quantize(normal(gen(3), 24, 64))
+    y, clean = hb.int8_gemm(x, w), hb.int8_gemm(x[[0, 3]].contiguous(), w)
+    assert torch.equal(y[[0, 3]], clean)
+    assert not torch.isfinite(y[1:3]).any()
+
+
+def check_product(hb, x, w, bias, y):
+    """The sum is exact; converting it, scaling by the token and scaling by the channel with the bias added are a rounding to FP32 each, the
+    result's type one more (binary16 may be subnormal: half its smallest step)."""
+    qa, sa = int8_reference(x)
+    acc = torch.from_numpy(qa).cuda().double() @ w.q[:, :w.k].double().t()
+    prod = acc * torch.from_numpy(sa).cuda().double()[:, None] * w.scale.double()
+    ref = prod + (bias.double() if bias is not None else 0)
+    tol = 3 * u(torch.float32) * prod.abs() + (u(y.dtype) + 2 * u(torch.float32)) * ref.abs()
+    tol += 2.0 ** -25 if y.dtype == torch.float16 else 1e-44
+    assert (y.double() - ref).abs().le(tol).all(), ((y.double() - ref).abs() / tol).max()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 64, 256), (1, 1000, 777), (2, 130, 33), (7, 129, 4096), (16, 256, 512), (17, 300, 1000), (33, 128, 2000),
+                                   (64, 512, 640), (65, 200, 128), (100, 77, 9000), (128, 128, 128), (129, 257, 515), (300, 1111, 200), (513, 640, 1024),
+                                   (2048, 1536, 64), (1, 20000, 48), (20000, 16, 48)])
+def test_int8_gemm(hb, dtype, M, N, K):
+    g = gen(M * 7 + N * 3 + K)
+    x = (normal(g, M, K) * torch.exp(normal(g, M, 1))).to(dtype)
+    w = hb.int8_quantize(normal(g, N, K) * torch.exp(normal(g, N, 1)))
+    bias = normal(g, N) if (M + N + K) % 2 else None
+    y = hb.int8_gemm(x, w, bias=bias)
+    assert y.dtype == dtype and y.shape == (M, N)
+    check_product(hb, x, w, bias, y)
+    again = hb.int8_gemm(hb.int8_quantize(x), w, bias=bias, dtype=dtype)       # converted before: the same numbers
+    assert torch.equal(y, again)
+
+
+def test_int8_gemm_largest_sums_are_exact(hb):
+    """K = 131071 of largest magnitude in both operands: the sum is 127 * 127 * K, close to 2^31."""
+    K = 131071
+    w = hb.Int8Rows(torch.zeros(16, K + 1, dtype=torch.int8, device="cuda"), torch.ones(16, device="cuda"), K)
+    w.q[::2, :K], w.q[1::2, :K] = 127, -128
+    x = torch.full((9, K), 127.0, device="cuda")
+    y = hb.int8_gemm(x, w)
+    expect = torch.tensor([127.0 * 127 * K, -127.0 * 128 * K] * 8, dtype=torch.float64, device="cuda").float()
+    assert torch.equal(y, expect.expand(9, 16))
+    x8 = hb.Int8Rows(torch.full((130, K + 1), -128, dtype=torch.int8, device="cuda"), torch.ones(130, device="cuda"), K)
+    y = hb.int8_gemm(x8, w)
+    assert torch.equal(y, torch.tensor([-127.0 * 128 * K, 128.0 * 128 * K] * 8, dtype=torch.float64, device="cuda").float().expand(130, 16))
+
+
+@pytest.mark.parametrize("M", [1, 20, 200])
+def test_int8_gemm_views_types_and_what_lies_behind(hb, M):
+    g = gen(M)
+    K, N = 200, 96
+    wide = normal(g, M, K + 9)
+    x = wide[:, 3:3 + K]                                                       # unaligned rows of a larger matrix
+    w = hb.int8_quantize(normal(g, N, K))
+    w.q[:, K:] = 99                                                            # bytes behind the contraction are not read
+    bias = normal(g, N)
+    full = torch.full((M + 2, N + 7), 42.0, device="cuda")
+    out = full[1:M + 1, 2:N + 2]
+    assert hb.int8_gemm(x, w, bias=bias, out=out) is out
+    check_product(hb, x, w, bias, out)
+    rest = full.clone()
+    rest[1:M + 1, 2:N + 2] = 42.0
+    assert (rest == 42.0).all()
+    for t in (torch.bfloat16, torch.float16):
+        check_product(hb, x, w, bias, hb.int8_gemm(x, w, bias=bias, dtype=t))
+    assert hb.int8_gemm(hb.int8_quantize(x), w).dtype == torch.float32
+    rows = hb.Int8Rows(w.q[5:40], w.scale[5:40], K)                            # some of the channels
+    assert torch.equal(hb.int8_gemm(x, rows), hb.int8_gemm(x, w)[:, 5:40])
+
+
+def test_int8_gemm_of_nothing(hb):
+    w = hb.int8_quantize(normal(gen(0), 8, 32))
+    assert hb.int8_gemm(torch.empty(0, 32, device="cuda"), w).shape == (0, 8)
+    assert hb.int8_gemm(normal(gen(1), 3, 32), hb.int8_quantize(torch.empty(0, 32, device="cuda"))).shape == (3, 0)
+    no_terms = hb.Int8Rows(torch.zeros(8, 16, dtype=torch.int8, device="cuda"), torch.ones(8, device="cuda"), 0)
+    bias = normal(gen(2), 8)
+    x = torch.empty(3, 0, device="cuda", dtype=torch.bfloat16)
+    assert torch.equal(hb.int8_gemm(x, no_terms, bias=bias), bias.bfloat16().expand(3, 8))
+    assert not hb.int8_gemm(x, no_terms).any()
+
+
+def test_int8_refusals(hb):
+    x, w = normal(gen(0), 4, 32), hb.int8_quantize(normal(gen(1), 8, 32))
+    for bad in (lambda: hb.int8_gemm(x.double(), w), lambda: hb.int8_gemm(x[:, :30], w), lambda: hb.int8_gemm(x.t(), w), lambda: hb.int8_gemm(x, w, bias=x[0, :8].double()),
+                lambda: hb.int8_gemm(x, w, bias=x[0, :7]), lambda: hb.int8_gemm(x, w, out=torch.empty(4, 9, device="cuda")),
+                lambda: hb.int8_gemm(x, w, out=torch.empty(4, 8)), lambda: hb.int8_gemm(x, hb.Int8Rows(w.q.cpu(), w.scale, 32)),
+                lambda: hb.int8_gemm(x, hb.Int8Rows(w.q.float(), w.scale, 32)), lambda: hb.int8_gemm(x, hb.Int8Rows(w.q, w.scale[:7], 32)),
+                lambda: hb.int8_gemm(x, hb.Int8Rows(w.q, w.scale, 33)), lambda: hb.int8_quantize(x, 2), lambda: hb.int8_quantize(x.long()),
+                lambda: hb.int8_gemm(x, w, out=torch.empty(4, 8, device="cuda"), dtype=torch.float16), lambda: hb.int8_quantize(x[0])):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(hb.HbfpError) as e:                                     # a pitch that is no multiple of 16
+        hb.int8_gemm(x[:, :20].contiguous(), hb.Int8Rows(torch.zeros(8, 20, dtype=torch.int8, device="cuda"), w.scale, 20))
+    assert e.value.code == hb.ERR_ALIGNMENT
+    with pytest.raises(hb.HbfpError) as e:
+        hb.int8_gemm(torch.zeros(1, 131072, device="cuda"), hb.Int8Rows(torch.zeros(1, 131072, dtype=torch.int8, device="cuda"), w.scale[:1], 131072))
+    assert e.value.code == hb.ERR_UNSUPPORTED
+
+
+# ----------------------------------------------------------------------------- the cache
+
+
+def unpack(m, e):
+    """The values (float64) of the cache's arrays, by the documented layout."""
+    words = m.contiguous().view(torch.int32).long()
+    place = torch.tensor([4 * (i // 2) + 16 * (i % 2) for i in range(8)], device=m.device)
+    q = ((words[..., None] >> place) & 15) - 8
+    q = q.flatten(-2).unflatten(-1, (-1, 32))
+    return (q.double() * torch.exp2(e.double())[..., None]).flatten(-2)
+
+
+def pages_of(lengths, page, g, spare=3):
+    """A page table for sequences of these lengths, pages in random order, -1 behind each sequence's last page."""
+    per = [-(-max(n, 0) // page) for n in lengths]
+    order = torch.randperm(sum(per) + spare, generator=g, device="cuda").int()
+    table = torch.full((len(lengths), max(max(per), 1)), -1, dtype=torch.int32, device="cuda")
+    at = 0
+    for b, c in enumerate(per):
+        table[b, :c] = order[at:at + c]
+        at += c
+    return table, sum(per) + spare
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,D,page", [(1, 64, 16), (3, 96, 32), (2, 128, 64), (2, 256, 16)])
+def test_append_is_the_librarys_4_bit_format(hb, dtype, heads, D, page):
+    """Mantissas and exponents equal the oracle's conversion with 4 bits and blocks of 32; other rows stay as they were."""
+    g = gen(D + heads)
+    lengths, n = [n0 + 5 for n0 in (0, 13, 16, 31, 77)], 5
+    table, pages = pages_of(lengths, page, g)
+    cache = hb.kv4_alloc(pages, heads, page, D)
+    for t in (cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps):
+        t.fill_(0x5A)
+    x = (normal(g, len(lengths) * n, 2, heads, D) * torch.exp(3 * normal(g, 1, 2, heads, 1))).to(dtype)
+    x[2, :, :, :32] = 0                                                        # an all-zero block
+    k, v = x[:, 0], x[:, 1]                                                    # rows of a fused tensor
+    hb.kv4_append(cache, k, v, table, i32(lengths))
+    written = torch.zeros(pages, page, dtype=torch.bool, device="cuda")
+    for src, m, e in ((k, cache.k_mant, cache.k_exps), (v, cache.v_mant, cache.v_exps)):
+        q, s = oracle.quantize(np.ascontiguousarray(src.float().cpu().numpy().reshape(-1, D)), 1, oracle.Format(mant_bits=4, block=32))
+        want = (q.reshape(-1, D // 32, 32) * np.exp2(s.astype(np.float64))[..., None]).reshape(len(lengths), n, heads, D)
+        for b, L in enumerate(lengths):
+            for i in range(n):
+                p = L - n + i
+                pg, r = int(table[b, p // page]), p % page
+                written[pg, r] = True
+                assert np.array_equal(e[pg, :, r].cpu().numpy(), s.reshape(len(lengths), n, heads, D // 32)[b, i])
+                assert np.array_equal(unpack(m[pg, :, r], e[pg, :, r]).cpu().numpy(), want[b, i])
+        assert (m.transpose(1, 2)[~written] == 0x5A).all() and (e.transpose(1, 2)[~written] == 0x5A).all()
+    rk, rv = hb.kv4_read(cache, n, table, i32(lengths))
+    assert torch.equal(rv.double().cpu(), torch.from_numpy(want.reshape(-1, heads, D)))
+
+
+def test_append_largest_values_saturate(hb):
+    cache = hb.kv4_alloc(1, 1, 16, 64)
+    k = torch.zeros(1, 1, 64, device="cuda")
+    k[0, 0, :4] = torch.tensor([3.0e38, 7 * 2.0 ** 120, -3.0e38, 2.0 ** 120], device="cuda")
+    k[0, 0, 32:34] = torch.tensor([1e-44, 0.0], device="cuda")
+    hb.kv4_append(cache, k, k, i32([[0]]), i32([1]))
+    r, _ = hb.kv4_read(cache, 1, i32([[0]]), i32([1]))
+    top = 7 * 2.0 ** 120
+    assert r[0, 0, :4].tolist() == [top, top, -top, 2.0 ** 120] and not r[0, 0, 4:].any()
+
+
+def test_append_ragged_starts_padding_and_short_sequences(hb):
+    """Sequences of 0, 1, 4 and 2 new tokens, one of them longer than its length (its first rows have no position), two rows behind the last."""
+    g = gen(5)
+    lengths, starts, page, heads, D = [40, 1, 2, 18], [0, 0, 1, 5, 7], 16, 2, 64
+    table, pages = pages_of(lengths, page, g)
+    cache = hb.kv4_alloc(pages, heads, page, D)
+    for t in (cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps):
+        t.zero_()
+    k, v = normal(g, 9, heads, D), normal(g, 9, heads, D)
+    hb.kv4_append(cache, k, v, table, i32(lengths), starts=i32(starts))
+    back = unpack(cache.k_mant, cache.k_exps).transpose(1, 2)                  # [pages][page][heads][D]
+    used = torch.zeros(pages, page, dtype=torch.bool, device="cuda")
+    for b, row, p in ((1, 0, 0), (2, 3, 0), (2, 4, 1), (3, 5, 16), (3, 6, 17)):
+        pg = int(table[b, p // page])
+        used[pg, p % page] = True
+        step = torch.exp2(cache.k_exps[pg, :, p % page].double()).repeat_interleave(32, -1)
+        # half a step; the largest magnitude of a block lies below 8 steps and is stored as 7 at most
+        assert (back[pg, p % page] - k[row].double()).abs().le(step).all()
+    assert not (cache.k_mant.transpose(1, 2)[~used]).any()
+
+
+def test_cache_refusals(hb):
+    cache = hb.kv4_alloc(4, 2, 16, 64)
+    k, t, n = normal(gen(0), 3, 2, 64), i32([[0, 1], [2, -1], [3, -1]]), i32([3, 4, 5])
+    for bad in (lambda: hb.kv4_append(cache, k, k.half(), t, n), lambda: hb.kv4_append(cache, k, k[:2], t, n), lambda: hb.kv4_append(cache, k[:2], k[:2], t, n),
+                lambda: hb.kv4_append(cache, k[:, :1], k[:, :1], t, n), lambda: hb.kv4_append(cache, k, k, t.long(), n), lambda: hb.kv4_append(cache, k, k, t, n[:2]),
+                lambda: hb.kv4_append(cache, k, k, t, n, max_tokens=1), lambda: hb.kv4_append(cache, k, k, t, n, starts=i32([0, 1, 2])),
+                lambda: hb.kv4_append(cache, k.double(), k.double(), t, n), lambda: hb.kv4_append(cache, k, k, t.cpu(), n),
+                lambda: hb.kv4_append(cache, k.transpose(1, 2).contiguous().transpose(1, 2), k, t, n),
+                lambda: hb.kv4_append(hb.Kv4Cache(cache.k_mant, cache.k_exps, cache.v_mant, cache.k_mant), k, k, t, n),
+                lambda: hb.kv4_append(hb.Kv4Cache(cache.k_mant, cache.k_exps[:3], cache.v_mant, cache.v_exps), k, k, t, n),
+                lambda: hb.kv4_read(cache, -1, t, n), lambda: hb.kv4_attention(normal(gen(0), 3, 3, 64), cache, t, n), lambda: hb.kv4_attention(k, cache, t, n, window=-1),
+                lambda: hb.kv4_attention(k[:, :, :32], cache, t, n), lambda: hb.kv4_attention(k, cache, t, n, out=torch.empty(3, 2, 64, device="cuda").half()),
+                lambda: hb.kv4_attention(k, cache, t, n, out=torch.empty(2, 2, 64, device="cuda")), lambda: hb.kv4_attention(k[:2], cache, t, n)):
+        with pytest.raises(ValueError):
+            bad()
+
+
+# ----------------------------------------------------------------------------- attention
+
+
+def fill(hb, g, pages, heads, page, D):
+    """A cache with values in every row of every page."""
+    cache = hb.kv4_alloc(pages, heads, page, D)
+    rows = pages * page
+    k = normal(g, rows, heads, D) * torch.exp(normal(g, 1, heads, D) * 0.5)
+    hb.kv4_append(cache, k, normal(g, rows, heads, D), torch.arange(pages, dtype=torch.int32, device="cuda")[None], i32([rows]))
+    return cache
+
+
+def attend_reference(q, cache, table, lengths, ns, scale, window=0):
+    """(out, bound): the definition in 64 bits and the error that the kernel's arithmetic can leave in FP32.
+
+    With S = scale * sum |q k| of a row's largest score and A = sum p |v|: a score is a sum of D exact products in FP32, sixteen and a part of the
+    query at a time (each step no worse than 2^-22 of S) and scaled and reduced by the maximum, a rounding of S each; p's error is the score's, in
+    numerator and denominator, and 2^-21 of the exponentials; p is rounded to the parts its type has (u(bfloat16) to that power); the sum over the keys
+    is again FP32, sixteen at a time."""
+    D, page = q.shape[2], cache.k_mant.shape[2]
+    heads = cache.k_mant.shape[1]
+    G = q.shape[1] // heads
+    parts = {torch.bfloat16: 1, torch.float16: 2, torch.float32: 3}[q.dtype]
+    out, tol = torch.zeros(q.shape, dtype=torch.float64, device="cuda"), torch.zeros(q.shape, dtype=torch.float64, device="cuda")
+    row = 0
+    K, V = unpack(cache.k_mant, cache.k_exps), unpack(cache.v_mant, cache.v_exps)
+    for b, L in enumerate(lengths):
+        n = ns[b]
+        pos = torch.arange(L, device="cuda")
+        ids = table[b].long()[pos // page]
+        i = torch.arange(L - n, L, device="cuda")[:, None]
+        seen = (pos[None] <= i) & (i >= 0)
+        if window:
+            seen &= pos[None] > i - window
+        for h in range(heads):
+            k, v = K[ids, h, pos % page], V[ids, h, pos % page]
+            for hq in range(h * G, h * G + G):
+                x = q[row:row + n, hq].double()
+                s = (x @ k.t() * scale).masked_fill(~seen, -math.inf)
+                top = s.max(-1, keepdim=True).values if L else torch.zeros(n, 1, dtype=torch.float64, device="cuda")
+                p = torch.exp(s - torch.where(top.isfinite(), top, 0.0))
+                total = p.sum(-1, keepdim=True)
+                p = torch.where(total > 0, p / total, 0.0)
+                out[row:row + n, hq] = p @ v
+                if L:
+                    S = (x.abs() @ k.abs().t() * abs(scale)).masked_fill(~seen, 0.0).max(-1, keepdim=True).values
+                    A = p @ v.abs()
+                    err = 2 * S * ((parts * D / 16 + 8) * 2.0 ** -22) + 2.0 ** -20 + (L / 16 + 8) * 2.0 ** -22 + u(torch.bfloat16) ** parts
+                    tol[row:row + n, hq] = A * err
+        row += n
+    return out, tol + u(q.dtype) * out.abs() + (2.0 ** -25 if q.dtype == torch.float16 else 1e-40)
+
+
+def check_attention(hb, dtype, heads, group, D, page, lengths, ns, window=0, scale=None, ragged=False, seed=0):
+    g = gen(seed + D + page + sum(lengths))
+    table, pages = pages_of(lengths, page, g)
+    cache = fill(hb, g, pages, heads, page, D)
+    q = normal(g, sum(ns), heads * group, D).to(dtype)
+    kw = {}
+    if ragged:
+        kw["starts"] = i32([0] + list(np.cumsum(ns)))
+        kw["max_tokens"] = max(ns)
+    y = hb.kv4_attention(q, cache, table, i32(lengths), scale=scale, window=window, **kw)
+    ref, tol = attend_reference(q, cache, table, lengths, ns, scale if scale is not None else D ** -0.5, window)
+    assert y.dtype == dtype and y.shape == q.shape
+    assert (y.double() - ref).abs().le(tol).all(), ((y.double() - ref).abs() / tol).max()
+    return q, cache, table, y
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,page", [(64, 16), (96, 32), (128, 64), (256, 16)])
+@pytest.mark.parametrize("heads,group", [(1, 1), (2, 3), (1, 8), (2, 12)])
+def test_attention_one_token(hb, dtype, D, page, heads, group):
+    check_attention(hb, dtype, heads, group, D, page, [1, 2, 15, 16, 17, 33, 128, 129, 300, 0], [1] * 10)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+def test_attention_long_keys_are_split(hb, dtype, D):
+    """Sequences whose keys several CTAs share, next to short and empty ones."""
+    check_attention(hb, dtype, 2, 4, D, 64, [5000, 1, 0, 2049, 640, 31], [1] * 6)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,group,n", [(64, 1, 5), (96, 3, 5), (128, 4, 3), (128, 1, 40), (256, 2, 7), (256, 2, 40), (64, 7, 20)])
+def test_attention_several_queries(hb, dtype, D, group, n):
+    check_attention(hb, dtype, 2, group, D, 32, [n, n + 1, n + 15, 700], [n] * 4)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("window", [1, 2, 16, 100, 257])
+@pytest.mark.parametrize("n", [1, 6, 33])
+def test_attention_window(hb, dtype, window, n):
+    check_attention(hb, dtype, 2, 2, 128, 16, [n, 64 + n, 300 + n, 1000], [n] * 4, window=window)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_attention_ragged_tokens(hb, dtype):
+    """Sequences of 0 to 50 new tokens, rows behind the last sequence's left as they were, first rows without a position."""
+    lengths, ns = [30, 7, 100, 2, 400, 0], [3, 0, 50, 5, 1, 2]
+    g = gen(9)
+    table, pages = pages_of(lengths, 16, g)
+    cache = fill(hb, g, pages, 2, 16, 64)
+    rows = sum(ns)
+    q = normal(g, rows + 4, 6, 64).to(dtype)
+    out = torch.full_like(q, 9.0)
+    hb.kv4_attention(q, cache, table, i32(lengths), starts=i32([0] + list(np.cumsum(ns))), max_tokens=50, out=out)
+    ref, tol = attend_reference(q[:rows], cache, table, lengths, ns, 0.125)
+    assert (out[:rows].double() - ref).abs().le(tol).all()
+    assert (out[rows:] == 9.0).all()
+    assert not out[53:56].any()                                                # three rows of five at negative positions: they see nothing
+    assert not out[rows - 2:rows].any()                                        # an empty sequence's
+    again = hb.kv4_attention(q, cache, table, i32(lengths), starts=i32([0] + list(np.cumsum(ns))))
+    assert torch.equal(again[:rows], out[:rows])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_attention_strides(hb, dtype):
+    """Queries are a slice of a fused projection, the output a slice of a larger tensor."""
+    g = gen(3)
+    lengths = [200, 17, 64]
+    table, pages = pages_of(lengths, 32, g)
+    cache = fill(hb, g, pages, 2, 32, 128)
+    fused = normal(g, 3, 8 + 4, 128 + 1).to(dtype)
+    q = fused[:, 1:9, 1:]
+    big = torch.full((3, 10, 200), 5.0, dtype=dtype, device="cuda")
+    out = big[:, 1:9, 3:131]
+    hb.kv4_attention(q, cache, table, i32(lengths), out=out)
+    ref, tol = attend_reference(q, cache, table, lengths, [1] * 3, 128 ** -0.5)
+    assert (out.double() - ref).abs().le(tol).all()
+    big[:, 1:9, 3:131] = 5.0
+    assert (big == 5.0).all()
+
+
+def test_attention_scores_far_apart_and_one_key_taking_all(hb):
+    """Scores over hundreds: all weight on one key, the others underflow; the maximum moves often."""
+    for scale in (0.0, 3.0, -2.0, 1e-3):
+        check_attention(hb, torch.float32, 1, 2, 64, 16, [900, 5], [1, 1], scale=scale)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_ignores_what_no_row_sees(hb, D):
+    """Rows of the last page behind the length, never written: any bytes there, the same result."""
+    g = gen(4)
+    lengths = [37, 1, 70]
+    table, pages = pages_of(lengths, 32, g, spare=0)
+    cache = fill(hb, g, pages, 1, 32, D)
+    q = normal(g, 3, 4, D)
+    y = hb.kv4_attention(q, cache, table, i32(lengths))
+    for b, L in enumerate(lengths):
+        if L % 32:
+            pg = int(table[b, L // 32])
+            for t in (cache.k_mant, cache.v_mant):
+                t[pg, :, L % 32:] = 0xFF
+            for t in (cache.k_exps, cache.v_exps):
+                t[pg, :, L % 32:] = 127
+    assert torch.equal(hb.kv4_attention(q, cache, table, i32(lengths)), y)
+
+
+@pytest.mark.parametrize("lengths", [[5000, 3, 700], [90, 17, 64]])
+def test_attention_repeats_itself_and_runs_in_a_graph(hb, lengths):
+    """The same bits every time, on another stream, and from a graph replayed after lengths, queries and cache have changed in place."""
+    g = gen(8)
+    table, pages = pages_of([max(lengths)] * 3, 64, g)
+    cache = fill(hb, g, pages, 2, 64, 128)
+    q, n = normal(g, 3, 8, 128).bfloat16(), i32(lengths)
+    y = hb.kv4_attention(q, cache, table, n)
+    for _ in range(3):
+        assert torch.equal(hb.kv4_attention(q, cache, table, n), y)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        z = hb.kv4_attention(q, cache, table, n)
+    side.synchronize()
+    assert torch.equal(z, y)
+    graph, out = torch.cuda.CUDAGraph(), torch.empty_like(q)
+    k = normal(g, 3, 2, 128).bfloat16()
+    with torch.cuda.graph(graph):
+        hb.kv4_append(cache, k, k, table, n)
+        hb.kv4_attention(q, cache, table, n, out=out)
+    for step in (1, 2):
+        n.sub_(1).clamp_(min=0)
+        q.copy_(normal(g, 3, 8, 128))
+        k.copy_(normal(g, 3, 2, 128))
+        graph.replay()
+        ref, tol = attend_reference(q, cache, table, n.tolist(), [1] * 3, 128 ** -0.5)
+        assert (out.double() - ref).abs().le(tol).all()
+
+
+def test_two_graphs_keep_their_own_workspaces(hb):
+    """Two captured calls of different sizes replayed in turn and at the same time: each has the result it had alone."""
+    g = gen(12)
+    calls = []
+    for lengths, heads in (([3000, 100], 2), ([9000], 4)):
+        table, pages = pages_of(lengths, 64, g)
+        calls.append((normal(g, len(lengths), heads * 4, 128).half(), fill(hb, g, pages, heads, 64, 128), table, i32(lengths)))
+    want = [hb.kv4_attention(*c) for c in calls]
+    graphs, outs = [], []
+    for c in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(hb.kv4_attention(*c))
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(5):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for s, gr in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                gr.replay()
+                gr.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+def test_pages_and_lengths_out_of_range_are_left_out_and_reported(hb):
+    """Numbers in device memory cannot be refused by the call: keys of a page that is none are not seen, and the status says so."""
+    g = gen(6)
+    lengths = [60, 33]
+    table, pages = pages_of(lengths, 16, g, spare=0)
+    cache = fill(hb, g, pages, 1, 16, 64)
+    q = normal(g, 2, 2, 64)
+    good = hb.kv4_attention(q, cache, table, i32(lengths))
+    assert hb.device_status() == 0
+    bad = table.clone()
+    bad[0, 1] = pages
+    y = hb.kv4_attention(q, cache, bad, i32(lengths))
+    assert hb.device_status_rc() == (hb.ERR_INDEX, 1001)
+    assert torch.equal(y[1], good[1]) and torch.isfinite(y).all()
+    hb.kv4_append(cache, q[:, :1], q[:, :1], i32([[-5], [10 ** 6]]), i32([1, 1]))            # nothing is written
+    assert hb.device_status_rc() == (hb.ERR_INDEX, 1001)
+    assert torch.equal(hb.kv4_attention(q, cache, table, i32(lengths)), good)
+    hb.kv4_attention(q, cache, table, i32([60, 1000]))                                       # longer than the table
+    assert hb.device_status_rc() == (hb.ERR_INDEX, 1002)
+    y = hb.kv4_attention(q, cache, table, i32(lengths), starts=i32([0, 5, 1]), out=torch.full_like(q, 3.0))
+    assert hb.device_status_rc() == (hb.ERR_INDEX, 1002)
+    assert (y == 3.0).all()
+    assert hb.device_status_rc() == (hb.OK, 0)
+
+
+def test_offsets_beyond_32_bits(hb):
+    """A cache whose arrays pass 2^32 bytes: pages at its end are written, read and attended."""
+    pages, heads, page, D = 40000, 8, 256, 128                                 # 5.2 GB of mantissas each
+    free, _ = torch.cuda.mem_get_info()
+    if free < 16 << 30:
+        pytest.skip("not enough device memory")
+    cache = hb.kv4_alloc(pages, heads, page, D)
+    g = gen(7)
+    table, n = i32([[pages - 1, 0], [pages - 2, 39000]]), [300, 290]
+    k, v = normal(g, 600, heads, D), normal(g, 600, heads, D)
+    hb.kv4_append(cache, k, v, table, i32(n), starts=i32([0, 300, 590]), max_tokens=300)
+    rk, rv = hb.kv4_read(cache, 290, table, i32(n))
+    for x, r in ((k, rk), (v, rv)):
+        want = torch.cat([x[10:300], x[300:590]])
+        assert ((r - want).abs() <= want.unflatten(-1, (-1, 32)).abs().amax(-1, keepdim=True).div(4).expand(-1, -1, -1, 32).flatten(-2)).all()
+    q = normal(g, 2, heads * 2, D)
+    small = hb.Kv4Cache(*(t[[pages - 1, 0, pages - 2, 39000]].contiguous() for t in (cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps)))
+    y, z = hb.kv4_attention(q, cache, table, i32(n)), hb.kv4_attention(q, small, i32([[0, 1], [2, 3]]), i32(n))
+    assert torch.equal(y, z)
+
+
+# ----------------------------------------------------------------------------- together
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_served_attention_layer(hb, dtype):
+    """Prompt and three decode steps of an attention layer whose projections were trained in block floating point: product, write,
+    attention, product, with ragged prompts. Each step against the definition on that step's own inputs."""
+    from paper_1804_01526_b200.autograd import HbfpLinear
+    from paper_1804_01526_b200.serving import Int8Linear
+    torch.manual_seed(0)
+    width, heads, group, D, page = 256, 2, 2, 64, 16
+    qkv = Int8Linear.from_hbfp(HbfpLinear(width, (heads * group + 2 * heads) * D, tile=32))
+    proj = Int8Linear.from_hbfp(HbfpLinear(heads * group * D, width, tile=32, bias=False))
+    g = gen(1)
+    ns = [20, 1, 33]
+    table, pages = pages_of([n + 3 for n in ns], page, g)
+    cache = hb.kv4_alloc(pages, heads, page, D)
+    lengths, starts = list(ns), [0, 20, 21, 54]
+    for step in range(4):
+        rows = sum(ns)
+        x = normal(g, rows, width).to(dtype)
+        y = qkv(x)
+        check_product(hb, x, hb.Int8Rows(qkv.weight_q, qkv.weight_scale, width), qkv.bias, y)
+        y = y.view(rows, -1, D)
+        q, k, v = y[:, :heads * group], y[:, heads * group:heads * group + heads], y[:, heads * group + heads:]
+        kw = dict(starts=i32(starts), max_tokens=max(ns)) if step == 0 else {}
+        hb.kv4_append(cache, k, v, table, i32(lengths), **kw)
+        o = hb.kv4_attention(q, cache, table, i32(lengths), **kw)
+        ref, tol = attend_reference(q, cache, table, lengths, ns, D ** -0.5)
+        assert (o.double() - ref).abs().le(tol).all()
+        z = proj(o.flatten(1))
+        assert z.shape == (rows, width)
+        check_product(hb, o.flatten(1), hb.Int8Rows(proj.weight_q, proj.weight_scale, heads * group * D), None, z)
+        ns = [1, 1, 1]
+        lengths = [n + 1 for n in lengths]
+    assert proj(o.view(3, 1, -1)).shape == (3, 1, width)
