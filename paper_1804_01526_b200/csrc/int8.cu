@@ -17,88 +17,119 @@ namespace {
 // The scale of a row from its largest |x|, given as a bit pattern (so that NaN is larger than infinity, and infinity than any number).
 __device__ __forceinline__ float scale_of(uint32_t amax_bits) { return __fdiv_rn(__uint_as_float(amax_bits), 127.0f); }
 
-// How a row's values are divided by its scale: q = rint(x * inv), and where x is next to the border between two whole numbers the
-// remainder x - q * s decides (one FMA; next to a border it is a multiple of half an ulp of s and no more than s / 2 and a little,
-// so it is exact, and an approximate quotient can miss the right whole number by one at most).
+// How a row's values are divided by its scale: q = rint(x * inv) where the quotient is clear of the border between two whole numbers, by
+// more than the error of x * inv (2^-23 of 127 at most). Next to a border (one value in 5000) the remainder x - q * s decides: one FMA, and
+// exact there, since it is a multiple of half an ulp of s and no more than s / 2 and a little; the approximate quotient misses the right whole
+// number by one at most.
 struct Divider {
     float s, inv;
-    bool small;              // inv is no normal number: divide in binary64
+    bool small;              // inv is no normal number: the division is binary64's
     __device__ __forceinline__ explicit Divider(float scale) : s(scale), inv(0.f), small(false) {
         if (!(s > 0.f) || s > 3.0e38f) s = 0.f;              // an all-zero row, or one that holds an infinity or NaN: q = 0
         else if (s < 1.0e-37f) small = true;
         else inv = __frcp_rn(s);
     }
-    __device__ __forceinline__ int operator()(float x) const {
-        if (small) return max(-127, min(127, (int)rint((double)x / (double)s)));      // (such a scale is coarse: it may round down far)
+    __device__ __forceinline__ int exactly(float x) const {
         const float t = __fmaf_rn(x, inv, 12582912.0f);      // 1.5 * 2^23: rounds to the nearest whole number, halves to even
-        const float q = t - 12582912.0f;
-        const float r = __fmaf_rn(-q, s, x);
+        const float r = __fmaf_rn(12582912.0f - t, s, x);
         int n = __float_as_int(t) - 0x4B400000;
-        if (fabsf(r) + fabsf(r) >= s && s > 0.f && (fabsf(r) + fabsf(r) > s || (n & 1))) n += r > 0.f ? 1 : -1;
+        const float twice = fabsf(r) + fabsf(r);
+        if (s > 0.f && (twice > s || (twice == s && (n & 1)))) n += r > 0.f ? 1 : -1;
         return n;
+    }
+    // (a scale below 1e-37 is coarse: it may have been rounded down far)
+    __device__ __forceinline__ int coarsely(float x) const { return max(-127, min(127, (int)rint((double)x / (double)s))); }
+    __device__ __forceinline__ int operator()(float x) const { return small ? coarsely(x) : exactly(x); }
+    // Eight values as bytes (not where the scale is `small`).
+    __device__ __forceinline__ uint2 eight(const float (&x)[8]) const {
+        const uint64_t inv2 = pack2(__float_as_uint(inv), __float_as_uint(inv)), up = pack2(0x4B400000u, 0x4B400000u), minus = pack2(0xBF800000u, 0xBF800000u);
+        float far = 0.f;
+        uint32_t n[8];
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const uint64_t v = pack2(__float_as_uint(x[i]), __float_as_uint(x[i + 1]));
+            const uint64_t t = ffma2(v, inv2, up), off = ffma2(v, inv2, ffma2(t, minus, up));        // up - t = -q
+            float t0, t1, o0, o1;
+            unpack2(t, t0, t1);
+            unpack2(off, o0, o1);
+            n[i] = __float_as_uint(t0);
+            n[i + 1] = __float_as_uint(t1);
+            asm("max.f32 %0, %0, %1, %2;" : "+f"(far) : "f"(fabsf(o0)), "f"(fabsf(o1)));
+        }
+        if (!(far < 0.4999f)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) n[i] = (uint32_t)exactly(x[i]);
+        }
+        // (the low byte of 1.5 * 2^23 + q is that of q)
+        return make_uint2(__byte_perm(__byte_perm(n[0], n[1], 0x0040), __byte_perm(n[2], n[3], 0x0040), 0x5410),
+                          __byte_perm(__byte_perm(n[4], n[5], 0x0040), __byte_perm(n[6], n[7], 0x0040), 0x5410));
     }
 };
 
-__device__ __forceinline__ uint32_t pack_bytes(int a, int b, int c, int d) {
-    return __byte_perm(__byte_perm((uint32_t)a, (uint32_t)b, 0x0040), __byte_perm((uint32_t)c, (uint32_t)d, 0x0040), 0x5410);
-}
-
-// Rows of x [rows][k] to q [rows][pitch] (bytes beyond k zero) and scale [rows]. A CTA per row; the row stays in registers where it
-// has up to KEEP * 8 values per thread, longer rows are read again (from L2). Bound by reading x and writing q.
+// Rows of x [rows][k] to q [rows][pitch] (bytes beyond k zero) and scale [rows]. GROUP threads take a row (a warp needs no barrier); it stays
+// in their registers, in its own type, up to KEEP * 8 values each, longer rows are read again (from L2). Bound by reading x and writing q:
+// 8192 x 8192 FP32 49 us, 6.8 TB/s.
 constexpr int QR_KEEP = 4;
-template <class T, int THREADS>
-__global__ void __launch_bounds__(THREADS)
-int8_rows_kernel(const T* __restrict__ x, int64_t k, int64_t ld, bool vec, int8_t* __restrict__ q, int64_t pitch, float* __restrict__ scale) {
+template <class T, int GROUP>
+__global__ void __launch_bounds__(GROUP > 256 ? GROUP : 256, GROUP > 256 ? 2 : 4)
+int8_rows_kernel(const T* __restrict__ x, int64_t rows, int64_t k, int64_t ld, bool vec, int8_t* __restrict__ q, int64_t pitch, float* __restrict__ scale) {
     chain_start();
-    const int64_t row = blockIdx.x;
-    const T* src = x + row * ld;
-    const int64_t pieces = pitch / 8;                        // of eight values; the row ends inside one of the last two
-    float v[QR_KEEP][8];
-    uint32_t am = 0;
-    auto fetch = [&](int64_t i, float (&e)[8]) {
-        const int64_t at = 8 * i;
-        if (vec && at + 8 <= k) load8(src + at, e);
-        else load8_part(src + at, (int)max((int64_t)0, min((int64_t)8, k - at)), e);
+    constexpr int THREADS = GROUP > 256 ? GROUP : 256;
+    const int me = threadIdx.x % GROUP;
+    const int64_t row = (int64_t)blockIdx.x * (THREADS / GROUP) + threadIdx.x / GROUP;
+    if (GROUP <= 32 && row >= rows) return;                          // (whole warps; with larger groups they stay for the barrier)
+    const bool in = row < rows;
+    const T* src = x + (in ? row : 0) * ld;
+    const int pieces = in ? (int)(pitch / 8) : 0, whole = vec ? (int)(k / 8) : 0;      // of eight values; the row ends inside one of the last two
+    Eight<T> v[QR_KEEP];
+    auto fetch = [&](int i, Eight<T>& e) {
+        if (i < whole) e.load(src + 8 * (int64_t)i);
+        else e.load_part(src + 8 * (int64_t)i, (int)(k - 8 * (int64_t)i));
     };
 #pragma unroll
     for (int u = 0; u < QR_KEEP; ++u) {
-        const int64_t i = threadIdx.x + u * THREADS;
+        const int i = me + u * GROUP;
+        v[u].zero();
         if (i < pieces) fetch(i, v[u]);
-        else
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[u][e] = 0.f;
     }
+    uint32_t am = 0;
 #pragma unroll
-    for (int u = 0; u < QR_KEEP; ++u)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) am = max(am, __float_as_uint(v[u][e]) & 0x7fffffffu);
-    for (int64_t i = threadIdx.x + QR_KEEP * THREADS; i < pieces; i += THREADS) {
-        float w[8];
+    for (int u = 0; u < QR_KEEP; ++u) am = max(am, v[u].amax_bits());
+    for (int i = me + QR_KEEP * GROUP; i < pieces; i += GROUP) {
+        Eight<T> w;
         fetch(i, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) am = max(am, __float_as_uint(w[e]) & 0x7fffffffu);
+        am = max(am, w.amax_bits());
     }
     am = __reduce_max_sync(0xffffffffu, am);
-    __shared__ uint32_t part[THREADS / 32];
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = am;
-    __syncthreads();
+    if (GROUP > 32) {
+        constexpr int W = GROUP / 32;
+        __shared__ uint32_t part[THREADS / 32];
+        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = am;
+        __syncthreads();
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) am = max(am, part[w]);
+        for (int w = 0; w < W; ++w) am = max(am, part[threadIdx.x / GROUP * W + w]);
+    }
+    if (!in) return;
     const float s = scale_of(am);
-    if (threadIdx.x == 0) scale[row] = s;
+    if (me == 0) scale[row] = s;
     const Divider div(s);
     int8_t* dst = q + row * pitch;
-    auto put = [&](int64_t i, const float (&e)[8]) {
-        const uint32_t lo = pack_bytes(div(e[0]), div(e[1]), div(e[2]), div(e[3])), hi = pack_bytes(div(e[4]), div(e[5]), div(e[6]), div(e[7]));
-        *reinterpret_cast<uint2*>(dst + 8 * i) = make_uint2(lo, hi);
+    if (div.small) {
+        for (int64_t i = me; i < pitch; i += GROUP) dst[i] = i < k ? (int8_t)div.coarsely(to_f32(src[i])) : (int8_t)0;
+        return;
+    }
+    auto put = [&](int i, const Eight<T>& e) {
+        float f[8];
+        e.get(f);
+        *reinterpret_cast<uint2*>(dst + 8 * (int64_t)i) = div.eight(f);
     };
 #pragma unroll
     for (int u = 0; u < QR_KEEP; ++u) {
-        const int64_t i = threadIdx.x + u * THREADS;
+        const int i = me + u * GROUP;
         if (i < pieces) put(i, v[u]);
     }
-    for (int64_t i = threadIdx.x + QR_KEEP * THREADS; i < pieces; i += THREADS) {
-        float w[8];
+    for (int i = me + QR_KEEP * GROUP; i < pieces; i += GROUP) {
+        Eight<T> w;
         fetch(i, w);
         put(i, w);
     }
@@ -142,7 +173,70 @@ struct Int8Problem {
     void* y;
     int64_t ldy;
     int32_t* status;
+    int tma_out;                     // the result has a tensor map
 };
+
+// The way of a finished tile out of a warp: 32 rows (lane = row) x 128 bytes of the result at a time, scaled, the bias added and rounded, in
+// shared memory (16-byte piece j of row r at piece j ^ (r & 7), the swizzle of the tensor map: no two lanes meet in a bank), from where the
+// copy engine stores it and clips it at the matrix's edge. Stored by the lanes themselves, 32 bytes of 32 rows an instruction, the FP32 result
+// of 4096 x 4096 x 1024 took 30.6 us where the product without its stores takes 15.4. A result whose pitch or place is not a multiple of 16
+// bytes is copied out along its rows.
+constexpr int I8_BOX = 32 * 128;
+struct Int8Out {
+    const CUtensorMap* map;      // null: no tensor map can be made
+    void* y;
+    int64_t ldy;
+    int M, N;
+};
+// Half of a box for 16-bit types, all of it for FP32: columns j0 .. j0 + 31 of it.
+template <class T>
+__device__ __forceinline__ void int8_fill_box(unsigned char* box, int j0, const int (&v)[32], float sa, const float* sb, const float* bias) {
+    constexpr int V = 16 / sizeof(T);
+    const int lane = threadIdx.x & 31;
+    unsigned char* line = box + lane * 128;
+#pragma unroll
+    for (int j = 0; j < 32; j += V) {
+        float o[V];
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            const float4 s = *reinterpret_cast<const float4*>(sb + j + i), b = *reinterpret_cast<const float4*>(bias + j + i);
+            o[i] = __fmaf_rn((float)v[j + i] * sa, s.x, b.x);
+            o[i + 1] = __fmaf_rn((float)v[j + i + 1] * sa, s.y, b.y);
+            o[i + 2] = __fmaf_rn((float)v[j + i + 2] * sa, s.z, b.z);
+            o[i + 3] = __fmaf_rn((float)v[j + i + 3] * sa, s.w, b.w);
+        }
+        store_piece(reinterpret_cast<T*>(line + ((((j0 + j) / V) ^ (lane & 7)) << 4)), o);
+    }
+}
+// The box leaves; it may be filled again after int8_box_free.
+template <class T>
+__device__ __forceinline__ void int8_send_box(const Int8Out& out, unsigned char* box, int row0, int col0) {
+    const int lane = threadIdx.x & 31;
+    if (out.map) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0 && row0 < out.M && col0 < out.N) {
+            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+                         ::"l"(reinterpret_cast<uint64_t>(out.map)), "r"(smem_u32(box)), "r"(col0 * (int)sizeof(T)), "r"(row0) : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+        return;
+    }
+    __syncwarp();
+    constexpr int COLS = 128 / sizeof(T);
+    T* y = reinterpret_cast<T*>(out.y);
+    const int rows = min(32, out.M - row0);
+    for (int r = 0; r < rows; ++r)
+#pragma unroll
+        for (int c = lane; c < COLS; c += 32) {
+            const int at = c * (int)sizeof(T);
+            if (col0 + c < out.N) y[(int64_t)(row0 + r) * out.ldy + col0 + c] = *reinterpret_cast<const T*>(box + r * 128 + (((at >> 4) ^ (r & 7)) << 4) + (at & 15));
+        }
+}
+__device__ __forceinline__ void int8_box_free() {
+    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+}
 
 // One 128 x NT tile per CTA: TMA fills stages of 128 bytes of K, one thread issues the MMAs, four warps read the finished int32 sums
 // from tensor memory, scale them and store.
@@ -150,21 +244,22 @@ template <int NT>
 struct I8Cfg {
     static constexpr int STAGE = (TILE_M + NT) * STAGE_K;
     static constexpr int STAGES = 5;
-    static constexpr int SMEM = 1024 + STAGES * STAGE + 1024 + 8 * NT;
+    static constexpr int SMEM = 1024 + STAGES * STAGE + 4 * I8_BOX + 1024 + 8 * NT;
     static constexpr int THREADS = 192;
 };
 
 template <class T, int NT>
 __global__ void __launch_bounds__(I8Cfg<NT>::THREADS)
-int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const Int8Problem p) {
+int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapY, const Int8Problem p) {
     using C = I8Cfg<NT>;
     extern __shared__ unsigned char smem_dyn[];
     const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     unsigned char* sm = smem_dyn + (base - smem_u32(smem_dyn));
-    const uint32_t full_bar = base + C::STAGES * C::STAGE, empty_bar = full_bar + 8 * C::STAGES, done_bar = empty_bar + 8 * C::STAGES;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + C::STAGES * C::STAGE + 16 * C::STAGES + 8);
+    constexpr int BARS = C::STAGES * C::STAGE + 4 * I8_BOX;
+    const uint32_t full_bar = base + BARS, empty_bar = full_bar + 8 * C::STAGES, done_bar = empty_bar + 8 * C::STAGES;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + BARS + 16 * C::STAGES + 8);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    float* cols = reinterpret_cast<float*>(sm + C::STAGES * C::STAGE + 1024);         // [NT] channel scales, [NT] biases
+    float* cols = reinterpret_cast<float*>(sm + BARS + 1024);         // [NT] channel scales, [NT] biases
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int m0 = blockIdx.y * TILE_M, n0 = blockIdx.x * NT;
     const int steps = (p.K + STAGE_K - 1) / STAGE_K;
@@ -229,26 +324,19 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         asm volatile("bar.sync 1, 128;" ::: "memory");
         if (mbar_wait_warp(done_bar, 0, abort_flag, p.status, 175)) {
             tc_fence_after();
-            T* dst = reinterpret_cast<T*>(p.y) + (int64_t)row * p.ldy + n0;
-            const bool quad = (p.ldy & 3) == 0 && (reinterpret_cast<uintptr_t>(p.y) & (4 * sizeof(T) - 1)) == 0;
+            const Int8Out out{p.tma_out ? &mapY : nullptr, p.y, p.ldy, p.M, p.N};
+            unsigned char* box = sm + C::STAGES * C::STAGE + (warp - 2) * I8_BOX;
+            constexpr int BOX = 128 / sizeof(T);
 #pragma unroll
             for (int c = 0; c < NT; c += 32) {
                 int v[32];
                 tc_ld32(tmem_base + ((uint32_t)(quarter * 32) << 16) + c, v);
                 tc_wait_ld();
-                if (row < p.M)
-#pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        float y[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) y[i] = __fmaf_rn((float)v[j + i] * sa, cols[c + j + i], cols[NT + c + j + i]);
-                        if (quad && n0 + c + j + 4 <= p.N) store4(dst + c + j, y[0], y[1], y[2], y[3]);
-                        else
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (n0 + c + j + i < p.N) dst[c + j + i] = from_f32<T>(y[i]);
-                    }
+                if (c % BOX == 0) int8_box_free();
+                int8_fill_box<T>(box, c % BOX, v, sa, cols + c, cols + NT + c);
+                if ((c + 32) % BOX == 0) int8_send_box<T>(out, box, m0 + quarter * 32, n0 + c + 32 - BOX);
             }
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         }
     }
     tc_fence_before();
@@ -256,6 +344,173 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(NT) : "memory");
+    }
+}
+
+// ---- Two SMs per 256 x NT tile, for products of many tiles. Each CTA of a pair brings its own 128 rows of tokens and half of the
+// channels' rows, so a byte from L2 takes part in twice the products of the kernel above, which is bound by that (8192 cube 545 us).
+// Persistent: a pair goes through its share of the tiles, the finished tile is read, scaled and stored by eight warps of each CTA while
+// the MMAs fill the next accumulator of tensor memory. (16 384 operations per clock and SM: 16 KB + NT / 2 * 128 bytes per stage.)
+template <int NT>
+struct I8Pair {
+    static constexpr int A_BYTES = TILE_M * STAGE_K, B_BYTES = NT / 2 * STAGE_K, STAGE = A_BYTES + B_BYTES;
+    static constexpr int STAGES = NT == 256 ? 5 : 7, GROUPS = TMEM_COLS / NT;
+    static constexpr int EPI_WARPS = 8, COLS = NT / 2, THREADS = 64 + 32 * EPI_WARPS;      // two warps per lane quarter, half the columns each
+    static constexpr int SCALES = EPI_WARPS * 2 * COLS * 4;       // per epilogue warp: channel scales, biases
+    static constexpr int SMEM = 1024 + STAGES * STAGE + EPI_WARPS * I8_BOX + SCALES + 1024;
+    static_assert(SMEM <= 232448, "shared memory");
+};
+template <int NT>
+__device__ __forceinline__ constexpr uint32_t idesc_i8_two() {
+    return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(2 * TILE_M >> 4) << 24);
+}
+
+// Tile `w` of the traversal: groups of eight tile rows sweep across the channels, so that their panels are shared in L2.
+__device__ __forceinline__ void pair_tile(int w, int tiles_m, int tiles_n, int& m, int& n) {
+    constexpr int G = 8;
+    const int per = G * tiles_n, group = w / per, first = group * G, size = min(G, tiles_m - first), within = w - group * per;
+    n = within / size;
+    m = first + (within - n * size);
+}
+
+template <class T, int NT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(I8Pair<NT>::THREADS, 1)
+int8_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapY, const Int8Problem p,
+                 int tiles_m, int tiles_n) {
+    using C = I8Pair<NT>;
+    extern __shared__ unsigned char smem_dyn[];
+    const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+    unsigned char* sm = smem_dyn + (base - smem_u32(smem_dyn));
+    float* scales = reinterpret_cast<float*>(sm + C::STAGES * C::STAGE + C::EPI_WARPS * I8_BOX);
+    constexpr int BARS = C::STAGES * C::STAGE + C::EPI_WARPS * I8_BOX + C::SCALES;
+    const uint32_t full_bar = base + BARS;                   // leader: tiles of both CTAs landed
+    const uint32_t empty_bar = full_bar + 8 * C::STAGES;     // local: the MMAs have read the stage
+    const uint32_t tfull_bar = empty_bar + 8 * C::STAGES;    // local: accumulator complete
+    const uint32_t tempty_bar = tfull_bar + 8 * C::GROUPS;   // leader: accumulator read by the warps of both CTAs
+    const uint32_t done_bar = tempty_bar + 8 * C::GROUPS;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + BARS + 16 * C::STAGES + 16 * C::GROUPS + 8);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int cluster = (int)cluster_id_x(), nclusters = (int)cluster_count_x(), total = tiles_m * tiles_n;
+    const int steps = (p.K + STAGE_K - 1) / STAGE_K;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(full_bar + 8 * s, 1); mbar_init(empty_bar + 8 * s, 1); }
+        for (int g = 0; g < C::GROUPS; ++g) { mbar_init(tfull_bar + 8 * g, 1); mbar_init(tempty_bar + 8 * g, 2 * C::EPI_WARPS); }
+        mbar_init(done_bar, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_barrier();            // both CTAs' barriers and tensor memory exist before anyone signals across
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    chain_start();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            const uint32_t leader_full = map_to_rank(full_bar, 0);
+            uint32_t s = 0, ph = 0, it = 0;
+            bool ok = true;
+            for (int w = cluster; ok && w < total; w += nclusters) {
+                int tm, tn;
+                pair_tile(w, tiles_m, tiles_n, tm, tn);
+                const int my_m = tm * 2 * TILE_M + (int)rank * TILE_M, my_n = tn * NT + (int)rank * (NT / 2);
+                for (int k = 0; k < steps; ++k, ++it) {
+                    if (!mbar_wait(empty_bar + 8 * s, ph ^ 1, abort_flag, p.status, 181)) { ok = false; break; }
+                    if (rank == 0) mbar_expect_tx(full_bar + 8 * s, 2u * C::STAGE);
+                    const uint32_t at = base + s * C::STAGE;
+                    tma_load_2d_pair(at, &mapA, k * STAGE_K, my_m, leader_full + 8 * s, L2_EVICT_LAST);
+                    tma_load_2d_pair(at + C::A_BYTES, &mapB, k * STAGE_K, my_n, leader_full + 8 * s, L2_EVICT_NORMAL);
+                    if (++s == C::STAGES) { s = 0; ph ^= 1; }
+                }
+            }
+            // the leader waits for the tiles of both CTAs that nobody may have waited for
+            if (rank == 0)
+                for (uint32_t back = min(it, (uint32_t)C::STAGES); back > 0; --back) {
+                    if (s == 0) { s = C::STAGES - 1; ph ^= 1; } else { --s; }
+                    mbar_wait(full_bar + 8 * s, ph, abort_flag, p.status, 182, false);
+                }
+        }
+    } else if (warp == 1) {
+        if (rank == 0 && elect_one()) {
+            uint32_t s = 0, ph = 0, g = 0, gph = 1;
+            bool ok = true;
+            for (int w = cluster; ok && w < total; w += nclusters) {
+                if (!mbar_wait(tempty_bar + 8 * g, gph, abort_flag, p.status, 183)) break;
+                tc_fence_after();
+                for (int k = 0; k < steps; ++k) {
+                    if (!mbar_wait(full_bar + 8 * s, ph, abort_flag, p.status, 184)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint64_t a = smem_desc_sw128(base + s * C::STAGE), b = smem_desc_sw128(base + s * C::STAGE + C::A_BYTES);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) tc_mma_i8_pair(tmem_base + g * NT, a + 2 * q, b + 2 * q, idesc_i8_two<NT>(), k > 0 || q > 0);
+                    tc_commit_pair(empty_bar + 8 * s, 3);
+                    if (++s == C::STAGES) { s = 0; ph ^= 1; }
+                }
+                if (ok) tc_commit_pair(tfull_bar + 8 * g, 3);
+                if (++g == C::GROUPS) { g = 0; gph ^= 1; }
+            }
+            tc_commit_pair(done_bar, 1);
+            mbar_wait(done_bar, 0, abort_flag, p.status, 185, false);
+        }
+    } else {
+        const int e = warp - 2, quarter = warp & 3, half = e >> 2;
+        float* sb = scales + e * 2 * C::COLS;
+        unsigned char* box = sm + C::STAGES * C::STAGE + e * I8_BOX;
+        const uint32_t tempty_leader = map_to_rank(tempty_bar, 0);
+        const Int8Out out{p.tma_out ? &mapY : nullptr, p.y, p.ldy, p.M, p.N};
+        constexpr int BOX = 128 / sizeof(T);
+        uint32_t g = 0, gph = 0;
+        for (int w = cluster; w < total; w += nclusters) {
+            int tm, tn;
+            pair_tile(w, tiles_m, tiles_n, tm, tn);
+            const int row = tm * 2 * TILE_M + (int)rank * TILE_M + quarter * 32 + lane, n0 = tn * NT + half * C::COLS;
+            __syncwarp();
+            for (int i = lane; i < C::COLS; i += 32) {
+                sb[i] = n0 + i < p.N ? __ldg(p.sb + n0 + i) : 0.f;
+                sb[C::COLS + i] = p.bias && n0 + i < p.N ? __ldg(p.bias + n0 + i) : 0.f;
+            }
+            const float sa = row < p.M ? __ldg(p.sa + row) : 0.f;
+            __syncwarp();
+            if (!mbar_wait_warp_fast(tfull_bar + 8 * g, gph, abort_flag, p.status, 186)) break;
+            tc_fence_after();
+            const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + g * NT + half * C::COLS;
+            constexpr int CH = 32;
+            int v[2][CH];
+            tc_ld32(taddr, v[0]);
+#pragma unroll
+            for (int c = 0; c < C::COLS; c += CH) {
+                tc_wait_ld();
+                if (c + CH < C::COLS) tc_ld32(taddr + c + CH, v[(c / CH + 1) & 1]);
+                else {
+                    // all of the accumulator is in registers: it is handed back before the last columns are scaled
+                    tc_fence_before();
+                    mbar_arrive_cluster_elect(tempty_leader + 8 * g);
+                }
+                const int(&x)[CH] = v[(c / CH) & 1];
+                if (c % BOX == 0) int8_box_free();
+                int8_fill_box<T>(box, c % BOX, x, sa, sb + c, sb + C::COLS + c);
+                if ((c + CH) % BOX == 0) int8_send_box<T>(out, box, row - lane, n0 + c + CH - BOX);
+            }
+            if (++g == C::GROUPS) { g = 0; gph ^= 1; }
+        }
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    // neither CTA leaves while the other can still signal its barriers
+    tc_fence_before();
+    __syncthreads();
+    cluster_barrier();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
     }
 }
 
@@ -275,8 +530,15 @@ int quantize_rows(const T* x, int64_t rows, int64_t k, int64_t ld, int8_t* q, in
     const bool vec = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && ld * sizeof(T) % 16 == 0;
     if (rows == 0) return HBFP_OK;
     const int64_t bytes = rows * k * (int64_t)sizeof(T);
-    if (pitch / 8 <= 64 * QR_KEEP) launch_streamed(bytes, int8_rows_kernel<T, 64>, (unsigned)rows, 64, 0, st, x, k, ld, vec, q, pitch, scale);
-    else launch_streamed(bytes, int8_rows_kernel<T, 256>, (unsigned)rows, 256, 0, st, x, k, ld, vec, q, pitch, scale);
+    auto launch = [&](auto kernel, int group) {
+        const int threads = group > 256 ? group : 256, per = threads / group;
+        launch_streamed(bytes, kernel, (unsigned)((rows + per - 1) / per), threads, 0, st, x, rows, k, ld, vec, q, pitch, scale);
+    };
+    // as few threads as keep the row in registers
+    if (pitch <= 32 * 8 * QR_KEEP) launch(int8_rows_kernel<T, 32>, 32);
+    else if (pitch <= 128 * 8 * QR_KEEP) launch(int8_rows_kernel<T, 128>, 128);
+    else if (pitch <= 256 * 8 * QR_KEEP) launch(int8_rows_kernel<T, 256>, 256);
+    else launch(int8_rows_kernel<T, 512>, 512);
     return launch_status();
 }
 
@@ -288,20 +550,69 @@ int quantize_any(const T* x, int64_t d0, int64_t d1, int64_t ld, int axis, int8_
     return launch_status();
 }
 
+// Tensor map of the result in boxes of 32 rows x 128 bytes, where its pitch and place allow one.
 template <class T>
-int product(const Int8Problem& p, const int8_t* a, int64_t lda, const int8_t* b, int64_t ldb, cudaStream_t st) {
+int map_result(Int8Problem& p, CUtensorMap* m) {
+    p.tma_out = p.ldy * (int64_t)sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(p.y) & 15) == 0;
+    if (!p.tma_out) { *m = CUtensorMap{}; return HBFP_OK; }
+    return make_map(m, p.y, (uint64_t)p.N * sizeof(T), p.M, p.ldy * sizeof(T), 128, 32, true);
+}
+
+template <class T, int NT>
+int launch_pair(Int8Problem p, const int8_t* a, int64_t lda, const int8_t* b, int64_t ldb, cudaStream_t st) {
+    using C = I8Pair<NT>;
+    CUtensorMap mA, mB, mY;
+    int rc = make_map(&mA, a, p.K, p.M, lda, STAGE_K, TILE_M, true);
+    if (!rc) rc = make_map(&mB, b, p.K, p.N, ldb, STAGE_K, NT / 2, true);
+    if (!rc) rc = map_result<T>(p, &mY);
+    if (!rc) rc = allow_shared<int8_pair_kernel<T, NT>>(C::SMEM);
+    if (rc) return rc;
+    const int tiles_m = (p.M + 2 * TILE_M - 1) / (2 * TILE_M), tiles_n = (p.N + NT - 1) / NT;
+    const int64_t tiles = (int64_t)tiles_m * tiles_n;
+    if (tiles >= (1ll << 30)) return HBFP_ERR_UNSUPPORTED;
+    // pairs that can be resident at once: the tiles are dealt out by their number
+    static std::atomic<int> resident[MAX_DEVICES];
+    const int dev = current_device();
+    if (dev < 0) return HBFP_ERR_CUDA;
+    int pairs = resident[dev].load(std::memory_order_acquire);
+    if (!pairs) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(2 * (unsigned)sm_count());
+        cfg.blockDim = dim3(C::THREADS);
+        cfg.dynamicSmemBytes = C::SMEM;
+        HBFP_CUDA_OK(cudaOccupancyMaxActiveClusters(&pairs, int8_pair_kernel<T, NT>, &cfg));
+        if (pairs < 1) return HBFP_ERR_CUDA;
+        resident[dev].store(pairs, std::memory_order_release);
+    }
+    launch_chained(int8_pair_kernel<T, NT>, dim3(2 * (unsigned)(tiles < pairs ? tiles : pairs)), C::THREADS, C::SMEM, st, mA, mB, mY, p, tiles_m, tiles_n);
+    note_product(st);
+    return launch_status();
+}
+// Enough 256 x 128 tiles to give every pair of SMs one.
+bool pair_eligible(int64_t M, int64_t N) { return M > 128 && (M + 255) / 256 * ((N + 127) / 128) >= 74; }
+
+template <class T>
+int product(Int8Problem p, const int8_t* a, int64_t lda, const int8_t* b, int64_t ldb, cudaStream_t st) {
     if (p.K == 0) {
         launch_chained(int8_no_terms_kernel<T>, (unsigned)(((int64_t)p.M * p.N + 255) / 256 < 148 * 8 ? ((int64_t)p.M * p.N + 255) / 256 : 148 * 8), 256, 0, st, p.bias,
                        static_cast<T*>(p.y), (int64_t)p.M, (int64_t)p.N, p.ldy);
         return launch_status();
     }
+    if (pair_eligible(p.M, p.N)) {
+        // 128 channels where the tiles fill the pairs that much better (such a tile takes 0.6 of the time of one of 256: 4096 cube 53.1 / 46.7 us
+        // in 7 rounds of the one and 4 of the other)
+        const int64_t tiles = (int64_t)((p.M + 255) / 256) * ((p.N + 255) / 256), halves = (int64_t)((p.M + 255) / 256) * ((p.N + 127) / 128);
+        if ((halves + 73) / 74 * 6 < (tiles + 73) / 74 * 10) return launch_pair<T, 128>(p, a, lda, b, ldb, st);
+        return launch_pair<T, 256>(p, a, lda, b, ldb, st);
+    }
     constexpr int NT = 128;
-    CUtensorMap mA, mB;
+    CUtensorMap mA, mB, mY;
     int rc = make_map(&mA, a, p.K, p.M, lda, STAGE_K, TILE_M, true);
     if (!rc) rc = make_map(&mB, b, p.K, p.N, ldb, STAGE_K, NT, true);
+    if (!rc) rc = map_result<T>(p, &mY);
     if (!rc) rc = allow_shared<int8_gemm_kernel<T, NT>>(I8Cfg<NT>::SMEM);
     if (rc) return rc;
-    launch_chained(int8_gemm_kernel<T, NT>, dim3((p.N + NT - 1) / NT, (p.M + TILE_M - 1) / TILE_M), I8Cfg<NT>::THREADS, I8Cfg<NT>::SMEM, st, mA, mB, p);
+    launch_chained(int8_gemm_kernel<T, NT>, dim3((p.N + NT - 1) / NT, (p.M + TILE_M - 1) / TILE_M), I8Cfg<NT>::THREADS, I8Cfg<NT>::SMEM, st, mA, mB, mY, p);
     note_product(st);
     return launch_status();
 }
@@ -318,7 +629,7 @@ int launch_int8_quantize(const void* x, int dtype, int64_t d0, int64_t d1, int64
 
 int launch_int8_gemm(int64_t M, int64_t N, int64_t K, const int8_t* a, int64_t lda, const float* sa, const int8_t* b, int64_t ldb, const float* sb,
                      const float* bias, void* y, int dtype, int64_t ldy, cudaStream_t st) {
-    Int8Problem p{(int)M, (int)N, (int)K, sa, sb, bias, y, ldy, device_status_word()};
+    Int8Problem p{(int)M, (int)N, (int)K, sa, sb, bias, y, ldy, device_status_word(), 0};
     if (!p.status) return HBFP_ERR_CUDA;
     if (dtype == HBFP_F32) return product<float>(p, a, lda, b, ldb, st);
     if (dtype == HBFP_BF16) return product<__nv_bfloat16>(p, a, lda, b, ldb, st);

@@ -448,10 +448,10 @@ __device__ __forceinline__ int2 ka_units(const Kv4Attend& a, const Kv4Seq& s) {
     return make_int2(max(1, (r.hi - r.lo + KaDim<D>::UNIT - 1) / KaDim<D>::UNIT), tiles);
 }
 // Units of all sequences and of those before each thread's share of them, by all threads of the CTA.
-template <int D, int NT>
+template <int D, int NT, int WARPS>
 __device__ __forceinline__ void ka_scan(const Kv4Attend& a, int& total, int& before, int& b0, int& b1) {
-    __shared__ int sums[KA_WARPS];
-    const int per = (a.c.sequences + KA_THREADS - 1) / KA_THREADS;
+    __shared__ int sums[WARPS];
+    const int per = (a.c.sequences + 32 * WARPS - 1) / (32 * WARPS);
     b0 = min(a.c.sequences, (int)threadIdx.x * per);
     b1 = min(a.c.sequences, b0 + per);
     int own = 0;
@@ -470,7 +470,7 @@ __device__ __forceinline__ void ka_scan(const Kv4Attend& a, int& total, int& bef
     total = 0;
     before = x - own;
 #pragma unroll
-    for (int w = 0; w < KA_WARPS; ++w) {
+    for (int w = 0; w < WARPS; ++w) {
         if (w < (int)(threadIdx.x >> 5)) before += sums[w];
         total += sums[w];
     }
@@ -483,7 +483,7 @@ kv4_attend_split_kernel(const Kv4Attend a) {
     __shared__ int found[2];
     chain_start();
     int total, before, b0, b1;
-    ka_scan<D, NT>(a, total, before, b0, b1);
+    ka_scan<D, NT, KA_WARPS>(a, total, before, b0, b1);
     const int ctas = min(a.ctas, total), cta = blockIdx.x;
     if (cta >= ctas) return;
     int u = (int)((int64_t)total * cta / ctas);
@@ -515,16 +515,20 @@ kv4_attend_split_kernel(const Kv4Attend a) {
     }
 }
 
-// The parts of the tiles that were split, joined in ascending order of their keys. A CTA per tile.
+// The parts of the tiles that were split, joined in ascending order of their keys. A CTA takes `each` rows of a tile, one after the
+// other; groups of dim / 4 threads share a row's parts, and their sums are added up in the order of the groups.
+constexpr int KJ_THREADS = 256;
 template <int D, int NT, class T>
-__global__ void __launch_bounds__(KA_THREADS)
-kv4_join_kernel(const Kv4Attend a) {
-    constexpr int RT = 8 * NT;
+__global__ void __launch_bounds__(KJ_THREADS)
+kv4_join_kernel(const Kv4Attend a, int each) {
+    constexpr int RT = 8 * NT, LANES = D / 4, GROUPS = KJ_THREADS / LANES;
     __shared__ int found[2];
+    __shared__ float4 sums[GROUPS][LANES];
+    __shared__ float weights[GROUPS];
     chain_start();
-    const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x;
+    const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x / (RT / each), row0 = blockIdx.x % (RT / each) * each;
     int total, before, b0, b1;
-    ka_scan<D, NT>(a, total, before, b0, b1);
+    ka_scan<D, NT, KJ_THREADS / 32>(a, total, before, b0, b1);
     const Kv4Seq s = kv4_seq(a.c, b);
     const int2 x = ka_units<D, NT>(a, s);
     const int item = tile * a.c.heads + h;
@@ -541,26 +545,47 @@ kv4_join_kernel(const Kv4Attend a) {
     const int first = found[0] + item * x.x;
     const int c0 = (int)(((int64_t)(first + 1) * ctas - 1) / total), c1 = (int)(((int64_t)(first + x.x) * ctas - 1) / total);
     if (c0 == c1) return;
-    const int rows = min(RT, s.n * a.group - tile * RT);
+    const int rows = min(RT, s.n * a.group - tile * RT), group = threadIdx.x / LANES, d = 4 * (threadIdx.x % LANES), lane = threadIdx.x & 31;
     const float2* ml = reinterpret_cast<const float2*>(a.partial + (int64_t)2 * a.ctas * RT * D);
-    for (int i = threadIdx.x; i < rows * (D / 4); i += KA_THREADS) {
-        const int r = i / (D / 4), d = 4 * (i - r * (D / 4));
-        float top = -INFINITY, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int c = c0; c <= c1; ++c) top = fmaxf(top, ml[(int64_t)(2 * c + (c == c0)) * RT + r].x);
-        if (top != -INFINITY)
-            for (int c = c0; c <= c1; ++c) {
-                const int64_t at = (int64_t)(2 * c + (c == c0)) * RT + r;
-                const float2 y = ml[at];
-                const float f = ka_exp2(y.x - top);
-                const float4 w = *reinterpret_cast<const float4*>(a.partial + at * D + d);
-                sum += f * y.y;
-                v[0] += f * w.x; v[1] += f * w.y; v[2] += f * w.z; v[3] += f * w.w;
-            }
-        const float inv = sum > 0.f ? __frcp_rn(sum) : 0.f;
-        const int query = (tile * RT + r) / a.group, gh = tile * RT + r - query * a.group;
-        T* dst = reinterpret_cast<T*>(a.out) + (s.first + query) * a.os.token + (h * a.group + gh) * a.os.head + d;
+    for (int r = row0; r < min(rows, row0 + each); ++r) {
+        auto place = [&](int c) { return (int64_t)(2 * c + (c == c0)) * RT + r; };
+        float top = -INFINITY;
+        for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, ml[place(c)].x);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) dst[e] = from_f32<T>(v[e] * inv);
+        for (int k = 1; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+        float sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (top != -INFINITY && group < GROUPS) {
+#pragma unroll 4
+            for (int c = c0 + group; c <= c1; c += GROUPS) {
+                const float2 y = ml[place(c)];
+                const float4 w = *reinterpret_cast<const float4*>(a.partial + place(c) * D + d);
+                const float f = ka_exp2(y.x - top);
+                sum += f * y.y;
+                v.x += f * w.x; v.y += f * w.y; v.z += f * w.z; v.w += f * w.w;
+            }
+        }
+        __syncthreads();                                                  // the row before has been stored
+        if (group < GROUPS) {
+            sums[group][threadIdx.x % LANES] = v;
+            if (d == 0) weights[group] = sum;
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+            for (int k = 1; k < GROUPS; ++k) {
+                const float4 w = sums[k][threadIdx.x];
+                sum += weights[k];
+                v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+            }
+            const float inv = sum > 0.f ? __frcp_rn(sum) : 0.f;
+            const int query = (tile * RT + r) / a.group, gh = tile * RT + r - query * a.group;
+            T* dst = reinterpret_cast<T*>(a.out) + (s.first + query) * a.os.token + (h * a.group + gh) * a.os.head + d;
+            dst[0] = from_f32<T>(v.x * inv);
+            dst[1] = from_f32<T>(v.y * inv);
+            dst[2] = from_f32<T>(v.z * inv);
+            dst[3] = from_f32<T>(v.w * inv);
+        }
     }
 }
 
@@ -602,7 +627,9 @@ int ka_launch(Kv4Attend a, cudaStream_t st, size_t* bytes) {
     }
     a.ctas = ctas;
     launch_chained(kv4_attend_split_kernel<D, NP, NT, T>, dim3((unsigned)ctas), KA_THREADS, SMEM, st, a);
-    launch_chained(kv4_join_kernel<D, NT, T>, grid, KA_THREADS, 0, st, a);
+    // few tiles have many parts each: a CTA per row
+    const int each = items < 256 ? 1 : 8;
+    launch_chained(kv4_join_kernel<D, NT, T>, dim3(grid.x * (RT / each), grid.y, grid.z), KJ_THREADS, 0, st, a, each);
     return launch_status();
 }
 

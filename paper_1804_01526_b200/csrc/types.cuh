@@ -61,11 +61,75 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b, const __half*) {
     const __half2 v = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-// Four neighbouring elements; p must be aligned to four elements.
-__device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
+__device__ __forceinline__ void unpack_pair(uint32_t w, float& a, float& b, const __nv_bfloat16*) {
+    a = __uint_as_float(w << 16);
+    b = __uint_as_float(w & 0xFFFF0000u);
+}
+__device__ __forceinline__ void unpack_pair(uint32_t w, float& a, float& b, const __half*) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    a = f.x;
+    b = f.y;
+}
+
+// Eight neighbouring elements held in their own type.
 template <class T>
-__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(pack_pair(a, b, p), pack_pair(c, d, p));
+struct Eight {
+    uint4 raw[sizeof(T) / 2];
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    __device__ __forceinline__ void load(const T* p) {                     // 16-byte aligned
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    }
+    __device__ __forceinline__ void load_part(const T* p, int n) {         // any alignment, elements from n on zero
+        T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < n ? p[i] : from_f32<T>(0.f);
+        uint32_t w[2 * sizeof(T)];
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(to_f32(e[i]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = pack_pair(to_f32(e[2 * i]), to_f32(e[2 * i + 1]), p);
+        }
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    }
+    // The largest magnitude as the bit pattern of an FP32 number (16-bit types: patterns of magnitudes are ordered as their values are, two at a time).
+    __device__ __forceinline__ uint32_t amax_bits() const {
+        if constexpr (sizeof(T) == 4) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) m = max(max(m, max(raw[i].x & 0x7fffffffu, raw[i].y & 0x7fffffffu)), max(raw[i].z & 0x7fffffffu, raw[i].w & 0x7fffffffu));
+            return m;
+        } else {
+            const uint32_t m = __vmaxu2(__vmaxu2(raw[0].x & 0x7fff7fffu, raw[0].y & 0x7fff7fffu), __vmaxu2(raw[0].z & 0x7fff7fffu, raw[0].w & 0x7fff7fffu));
+            float a, b;
+            unpack_pair(m, a, b, (const T*)nullptr);
+            return max(__float_as_uint(a), __float_as_uint(b));
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        if constexpr (sizeof(T) == 4) {
+            const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+        } else {
+            const uint32_t w[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) unpack_pair(w[i], v[2 * i], v[2 * i + 1], (const T*)nullptr);
+        }
+    }
+};
+
+// Sixteen bytes; p must be 16-byte aligned.
+__device__ __forceinline__ void store_piece(float* p, const float (&v)[4]) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+template <class T>
+__device__ __forceinline__ void store_piece(T* p, const float (&v)[8]) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_pair(v[0], v[1], p), pack_pair(v[2], v[3], p), pack_pair(v[4], v[5], p), pack_pair(v[6], v[7], p));
 }
 
 }  // namespace
