@@ -63,6 +63,7 @@ int attend(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int dtype, 
         a->c.status = device_status_word();
         if (!a->c.status) return HBFP_ERR_CUDA;
     }
+    if (kv4_prompt_eligible(*a)) return bytes ? (int)HBFP_OK : launch_kv4_prompt(*a, dtype, st);
     if (dtype == HBFP_F32) return launch_kv4_attend_f32(*a, st, bytes);
     if (dtype == HBFP_BF16) return launch_kv4_attend_bf16(*a, st, bytes);
     return launch_kv4_attend_f16(*a, st, bytes);

@@ -1,0 +1,422 @@
+// Attention of many query rows (prompts) over the 4-bit cache on the fifth-generation tensor cores.
+//
+// A CTA takes 128 rows, or two tiles of 128 where a query is one bfloat16 part, of one sequence and KV head: rows = queries times the
+// query heads of the KV head. Keys come in tiles of 128. Four warps unpack a tile's keys and values to bfloat16 (exact, see kv4_attend.cuh)
+// into swizzled shared memory, once for all rows; one thread issues S = Q K^T and O += P V; a warpgroup per row tile holds a row per thread:
+// it reads the scores from tensor memory, keeps the row's maximum and sum in FP32, and writes the probabilities back to tensor memory as the
+// bfloat16 operand of the second product (which takes it from there; V's tile is the operand with the values contiguous, keys down its rows).
+// With two row tiles the MMAs of one run while the other's softmax does; probabilities then lie in the place of their scores.
+//
+// Queries and probabilities have as many bfloat16 parts as their type has bits (1, 2 or 3 as in kv4_attend.cuh), each an MMA of its own.
+// The maximum is only moved, and O rescaled, when a row's scores exceed it by more than 2^8: probabilities up to 2^8 lose nothing in FP32 and
+// bfloat16, and the sum is divided out with the same maximum.
+//
+// Bound: per 128 keys and 256 rows 2048 cycles of MMA (bfloat16, 128 wide) and as many of exponentials.
+#include <cuda.h>
+
+#include <atomic>
+
+#include "kv4_attend.cuh"
+
+namespace hbfp {
+namespace {
+
+constexpr int KP_KEYS = 128;
+constexpr float KP_SLACK = 8.0f;
+
+template <int D, int NP> struct KpCfg {
+    static constexpr int QT = NP == 1 ? 2 : 1;                             // row tiles of a CTA
+    static constexpr int ROWS = 128 * QT, HALVES = D / 64;
+    static constexpr int TILE = HALVES * 16384;                            // 128 rows of D bfloat16, 128-byte columns swizzled
+    static constexpr int SOFT_WARPS = 4 * QT, FILL_WARPS = 4, THREADS = 32 * (SOFT_WARPS + FILL_WARPS + 1);
+    static constexpr int OFF_K = QT * NP * TILE, OFF_V = OFF_K + 2 * TILE, OFF_BAR = OFF_V + 2 * TILE;
+    static constexpr int SMEM = 1024 + OFF_BAR + 512;
+    static_assert(SMEM <= 232448, "shared memory");
+    // columns of tensor memory
+    static constexpr int S_COL = 0, O_COL = 128 * QT, P_COL = QT == 2 ? 0 : 256;     // scores and results of tile t: + 128 t; parts of P: + 64 p
+};
+
+__device__ __forceinline__ void kp_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// The same with A in tensor memory (two neighbours along K to a column).
+__device__ __forceinline__ void kp_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// FP32 accumulator, bfloat16 operands, M = 128; B_MN: the columns of B are contiguous, not its contraction.
+template <int N, bool B_MN>
+__device__ __forceinline__ constexpr uint32_t kp_idesc() {
+    return (1u << 4) | (1u << 7) | (1u << 10) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(N >> 3) << 17) | (8u << 24);
+}
+// Descriptor of a tile whose columns are contiguous: 64 of them (128 bytes, swizzled) by 8 rows of the contraction an atom, atoms 1024 bytes
+// apart along the contraction and 16384 along the columns.
+__device__ __forceinline__ uint64_t kp_desc_mn(uint32_t addr) {
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(16384 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+// One word of eight values as 16 bytes of bfloat16.
+__device__ __forceinline__ uint4 kp_unpack(uint32_t w, uint32_t scale, uint32_t offset) {
+    return make_uint4(ka_value(w, scale, offset), ka_value(w >> 4, scale, offset), ka_value(w >> 8, scale, offset), ka_value(w >> 12, scale, offset));
+}
+
+template <int D, int NP, class T>
+__global__ void __launch_bounds__(KpCfg<D, NP>::THREADS, 1)
+kv4_prompt_kernel(const Kv4Attend a) {
+    using C = KpCfg<D, NP>;
+    extern __shared__ unsigned char smem_dyn[];
+    const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+    unsigned char* sm = smem_dyn + (base - smem_u32(smem_dyn));
+    const uint32_t bars = base + C::OFF_BAR;
+    const uint32_t kfull = bars, vfull = bars + 16, kempty = bars + 32, vempty = bars + 48, sfull = bars + 64, pfull = bars + 80, odone = bars + 96, done = bars + 112;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + C::OFF_BAR + 128);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    volatile int* holes = reinterpret_cast<volatile int*>(tmem_slot + 4);        // [4 tiles][4 warps]: groups of sixteen keys that are not there
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    // the tiles with the most keys first
+    const int h = blockIdx.x % a.c.heads, b = blockIdx.x / a.c.heads, tile = gridDim.y - 1 - blockIdx.y;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(kfull + 8 * i, C::FILL_WARPS);
+            mbar_init(vfull + 8 * i, C::FILL_WARPS);
+            mbar_init(kempty + 8 * i, 1);
+            mbar_init(vempty + 8 * i, 1);
+            mbar_init(sfull + 8 * i, 1);
+            mbar_init(pfull + 8 * i, 4);
+            mbar_init(odone + 8 * i, 1);
+        }
+        mbar_init(done, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    constexpr int MMA_WARP = C::SOFT_WARPS + C::FILL_WARPS;
+    if (warp == MMA_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(TMEM_COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    chain_start();
+
+    const Kv4Seq seq = kv4_seq(a.c, b);
+    const int all = seq.n * a.group, r0 = tile * C::ROWS, rows = min(C::ROWS, all - r0);
+    if (rows > 0) {
+        const int first = seq.length - seq.n;                              // position of the first query
+        // keys [lo, hi): hi of the last row, lo of the first; tiles of keys for each row tile
+        const int hi = max(0, min(seq.length, first + (r0 + rows - 1) / a.group + 1));
+        const int lo = a.window ? max(0, first + r0 / a.group - a.window + 1) & ~15 : 0;
+        int n[C::QT], most = 0;
+#pragma unroll
+        for (int t = 0; t < C::QT; ++t) {
+            const int last = min(r0 + 128 * t + 127, r0 + rows - 1);
+            const int hi_t = 128 * t < rows ? max(0, min(seq.length, first + last / a.group + 1)) : 0;
+            n[t] = hi_t > lo ? (hi_t - lo + KP_KEYS - 1) / KP_KEYS : 0;
+            most = max(most, n[t]);
+        }
+        const float flip = a.scale2 < 0.f ? -1.f : 1.f, scale2 = fabsf(a.scale2);
+
+        // ---- the queries, in parts (a negative scale is a negative query)
+        const bool vec = ((reinterpret_cast<uintptr_t>(a.q) | (uintptr_t)((a.qs.token | a.qs.head) * (int64_t)sizeof(T))) & 15) == 0;
+        for (int i = threadIdx.x; i < C::ROWS * (D / 8); i += C::THREADS) {
+            const int r = i / (D / 8), c = i - r * (D / 8);
+            float e[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (r < rows) {
+                const int query = (r0 + r) / a.group, gh = r0 + r - query * a.group;
+                const T* src = reinterpret_cast<const T*>(a.q) + (seq.first + query) * a.qs.token + (h * a.group + gh) * a.qs.head + 8 * c;
+                if (vec) load8(src, e);
+                else load8_part(src, 8, e);
+            }
+            uint32_t x[4][NP];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ka_parts<NP>(flip * e[2 * j], flip * e[2 * j + 1], x[j]);
+            unsigned char* at = sm + (r >> 7) * C::TILE + (c >> 3) * 16384 + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
+#pragma unroll
+            for (int p = 0; p < NP; ++p) *reinterpret_cast<uint4*>(at + p * C::TILE) = make_uint4(x[0][p], x[1][p], x[2][p], x[3][p]);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
+
+        if (warp >= C::SOFT_WARPS && warp < MMA_WARP) {
+            // ------------------------------------------------------------ unpacking: 32 keys of a tile per warp, a block of 32 values a lane and load
+            constexpr int NBLK = D / 32, KPL = 32 / NBLK, LOADS = 32 / KPL;        // blocks of a row, keys of a load, loads of 32 keys
+            const int w = warp - C::SOFT_WARPS, blk = (lane >> 3) % NBLK, sub = (lane & 7) + 8 * ((lane >> 3) / NBLK);
+            uint4 kr[LOADS], vr[LOADS];
+            int ke[LOADS], ve[LOADS];
+            int64_t row[2];
+            int gone = 0;
+            auto find = [&](int j) {
+                gone = 0;
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const int p = lo + j * KP_KEYS + 32 * w + 16 * g;
+                    row[g] = -1;
+                    if (j < most && p < hi) {
+                        const int64_t page = kv4_page(a.c, b, p >> a.c.shift);
+                        if (page >= 0) row[g] = ((page * a.c.heads + h) << a.c.shift) + (p & (a.c.page - 1));
+                        else gone |= 1 << g;
+                    }
+                }
+            };
+            auto load = [&](const uint8_t* mant, const int8_t* exps, uint4 (&m)[LOADS], int (&e)[LOADS]) {
+#pragma unroll
+                for (int u = 0; u < LOADS; ++u) {
+                    const int key = KPL * u + sub;                          // of the warp's 32
+                    const int64_t at = (key >> 4) ? row[1] : row[0];
+                    m[u] = make_uint4(0u, 0u, 0u, 0u);
+                    e[u] = 0;
+                    if (at >= 0) {
+                        const int64_t line = at + (key & 15);
+                        m[u] = __ldg(reinterpret_cast<const uint4*>(mant + line * (D / 2)) + blk);
+                        e[u] = __ldg(exps + line * NBLK + blk);
+                    }
+                }
+            };
+            auto store = [&](unsigned char* to, const uint4 (&m)[LOADS], const int (&e)[LOADS]) {
+#pragma unroll
+                for (int u = 0; u < LOADS; ++u) {
+                    const int key = 32 * w + KPL * u + sub, x = kv4_exponent((int8_t)e[u]);
+                    const uint32_t scale = ka_scale(x, x), offset = ka_offset(scale);
+                    const uint32_t words[4] = {m[u].x, m[u].y, m[u].z, m[u].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int c = 4 * blk + i;
+                        *reinterpret_cast<uint4*>(to + (c >> 3) * 16384 + key * 128 + (((c & 7) ^ (key & 7)) << 4)) = kp_unpack(words[i], scale, offset);
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            };
+            find(0);
+            load(a.c.k_mant, a.c.k_exps, kr, ke);
+            load(a.c.v_mant, a.c.v_exps, vr, ve);
+            for (int j = 0; j < most; ++j) {
+                const int s = j & 1;
+                const uint32_t ph = (uint32_t)((j >> 1) & 1) ^ 1u;
+                if (!mbar_wait_warp(kempty + 8 * s, ph, abort_flag, a.c.status, 191)) break;
+                if (lane == 0) holes[(j & 3) * 4 + w] = gone;
+                store(sm + C::OFF_K + s * C::TILE, kr, ke);
+                if (lane == 0) mbar_arrive(kfull + 8 * s);
+                find(j + 1);
+                load(a.c.k_mant, a.c.k_exps, kr, ke);
+                if (!mbar_wait_warp(vempty + 8 * s, ph, abort_flag, a.c.status, 192)) break;
+                store(sm + C::OFF_V + s * C::TILE, vr, ve);
+                if (lane == 0) mbar_arrive(vfull + 8 * s);
+                load(a.c.v_mant, a.c.v_exps, vr, ve);
+            }
+        } else if (warp == MMA_WARP) {
+            // ------------------------------------------------------------ MMAs
+            if (elect_one()) {
+                auto scores = [&](int t, int j) {
+                    const uint32_t d = tmem + C::S_COL + 128 * t, kt = base + C::OFF_K + (j & 1) * C::TILE;
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                        for (int i = 0; i < D / 16; ++i) {
+                            const uint32_t off = (uint32_t)(i >> 2) * 16384u + (uint32_t)(i & 3) * 32u;
+                            kp_mma(d, smem_desc_sw128(base + (t * NP + p) * C::TILE + off), smem_desc_sw128(kt + off), kp_idesc<KP_KEYS, false>(), p < NP - 1 || i > 0);
+                        }
+                };
+                auto values = [&](int t, int j) {
+                    const uint32_t d = tmem + C::O_COL + 128 * t, pt = tmem + C::P_COL + 128 * t, vt = base + C::OFF_V + (j & 1) * C::TILE;
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                        for (int i = 0; i < KP_KEYS / 16; ++i)
+                            kp_mma_ts(d, pt + 64 * p + 8 * i, kp_desc_mn(vt + i * 2048), kp_idesc<D, true>(), j > 0 || p < NP - 1 || i > 0);
+                };
+                bool ok = most == 0 || mbar_wait(kfull, 0, abort_flag, a.c.status, 193);
+                if (ok && most > 0) {
+                    tc_fence_after();
+#pragma unroll
+                    for (int t = 0; t < C::QT; ++t)
+                        if (n[t] > 0) {
+                            scores(t, 0);
+                            tc_commit(sfull + 8 * t);
+                        }
+                    tc_commit(kempty);
+                }
+                for (int j = 0; ok && j < most; ++j) {
+                    const int s = j & 1, s1 = (j + 1) & 1;
+                    if (!mbar_wait(vfull + 8 * s, (uint32_t)((j >> 1) & 1), abort_flag, a.c.status, 194)) { ok = false; break; }
+                    if (j + 1 < most && !mbar_wait(kfull + 8 * s1, (uint32_t)(((j + 1) >> 1) & 1), abort_flag, a.c.status, 195)) { ok = false; break; }
+#pragma unroll
+                    for (int t = 0; t < C::QT; ++t) {
+                        if (!ok || j >= n[t]) continue;
+                        if (!mbar_wait(pfull + 8 * t, (uint32_t)(j & 1), abort_flag, a.c.status, 196)) { ok = false; continue; }
+                        tc_fence_after();
+                        values(t, j);
+                        if (j + 1 < n[t]) {
+                            scores(t, j + 1);
+                            tc_commit(sfull + 8 * t);
+                        } else {
+                            tc_commit(odone + 8 * t);
+                        }
+                    }
+                    if (!ok) break;
+                    tc_commit(vempty + 8 * s);
+                    if (j + 1 < most) tc_commit(kempty + 8 * s1);
+                }
+                tc_commit(done);
+                mbar_wait(done, 0, abort_flag, a.c.status, 197, false);
+            }
+        } else {
+            // ------------------------------------------------------------ softmax: a row per thread
+            const int t = warp >> 2, quarter = warp & 3, r = 128 * t + quarter * 32 + lane;
+            const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), sc = lanes + C::S_COL + 128 * t, oc = lanes + C::O_COL + 128 * t, pc = lanes + C::P_COL + 128 * t;
+            const int limit = first + (r0 + min(r, rows - 1)) / a.group, window = a.window ? a.window : 0x7fffffff;
+            // rows of this warp: the first's limit and the last's, for a look at whole tiles
+            const int limit0 = __reduce_min_sync(0xffffffffu, limit), limit1 = __reduce_max_sync(0xffffffffu, limit);
+            float m = -INFINITY, l = 0.f;
+            bool ok = true;
+            const int mine = t == 0 ? n[0] : n[C::QT - 1];
+            for (int j = 0; j < mine; ++j) {
+                if (!mbar_wait_warp_fast(sfull + 8 * t, (uint32_t)(j & 1), abort_flag, a.c.status, 198)) { ok = false; break; }
+                tc_fence_after();
+                const int pos = lo + j * KP_KEYS;
+                const int missing = holes[(j & 3) * 4] | holes[(j & 3) * 4 + 1] << 2 | holes[(j & 3) * 4 + 2] << 4 | holes[(j & 3) * 4 + 3] << 6;
+                const bool whole = pos + KP_KEYS - 1 <= limit0 && limit1 - pos < window && missing == 0;
+                // columns [from, to) of the tile are seen by this row
+                const int to = min(limit + 1, hi) - pos, from = limit - pos - window + 1;
+                auto seen = [&](int c) { return c >= from && c < to && !(missing >> (c >> 4) & 1); };
+                float top = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < KP_KEYS; c += 32) {
+                    uint32_t v[32];
+                    tc_ld32(sc + c, v);
+                    tc_wait_ld();
+                    if (!whole)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!seen(c + i)) v[i] = 0xFF800000u;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(__uint_as_float(v[i])), "f"(__uint_as_float(v[i + 1])));
+                }
+                const float top2 = top == -INFINITY ? top : top * scale2;
+                const bool move = top2 > m + KP_SLACK || (m == -INFINITY && top2 != -INFINITY);
+                if (__any_sync(0xffffffffu, move)) {
+                    const float f = move ? ka_exp2(m - top2) : 1.f;        // m = -inf: 0
+                    if (move) m = top2;
+                    l *= f;
+                    if (j > 0) {
+#pragma unroll
+                        for (int c = 0; c < D; c += 32) {
+                            uint32_t v[32];
+                            tc_ld32(oc + c, v);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+                            tc_st32(oc + c, v);
+                        }
+                        tc_wait_st();
+                    }
+                }
+                const float m_use = m == -INFINITY ? 0.f : m;
+                const uint64_t k2 = pack2(__float_as_uint(scale2), __float_as_uint(scale2)), m2 = pack2(__float_as_uint(-m_use), __float_as_uint(-m_use));
+                uint64_t sum = 0ull;
+#pragma unroll
+                for (int c = 0; c < KP_KEYS; c += 32) {
+                    uint32_t v[32], x[NP][16];
+                    tc_ld32(sc + c, v);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        float e0, e1;
+                        unpack2(ffma2(pack2(v[i], v[i + 1]), k2, m2), e0, e1);
+                        if (!whole) {
+                            if (!seen(c + i)) e0 = -INFINITY;
+                            if (!seen(c + i + 1)) e1 = -INFINITY;
+                        }
+                        e0 = ka_exp2(e0);
+                        e1 = ka_exp2(e1);
+                        sum = fadd2(sum, pack2(__float_as_uint(e0), __float_as_uint(e1)));
+                        uint32_t parts[NP];
+                        ka_parts<NP>(e0, e1, parts);
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) x[p][i / 2] = parts[p];
+                    }
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) tc_st16(pc + 64 * p + c / 2, x[p]);
+                }
+                float s0, s1;
+                unpack2(sum, s0, s1);
+                l += s0 + s1;
+                tc_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(pfull + 8 * t);
+            }
+            // ---- the row's result
+            if (ok && mine > 0) ok = mbar_wait_warp_fast(odone + 8 * t, 0, abort_flag, a.c.status, 199);
+            if (ok) {
+                tc_fence_after();
+                const float inv = l > 0.f ? __frcp_rn(l) : 0.f;            // a row that sees no key: zeros
+                const int query = (r0 + r) / a.group, gh = r0 + r - query * a.group;
+                T* dst = reinterpret_cast<T*>(a.out) + (seq.first + query) * a.os.token + (h * a.group + gh) * a.os.head;
+                constexpr int V = 16 / sizeof(T);
+                const bool pieces = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)((a.os.token | a.os.head) * (int64_t)sizeof(T))) & 15) == 0;
+#pragma unroll
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t v[32];
+                    if (mine > 0) {
+                        tc_ld32(oc + c, v);
+                        tc_wait_ld();
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = 0u;
+                    }
+                    if (r >= rows) continue;
+#pragma unroll
+                    for (int i = 0; i < 32; i += V) {
+                        float y[V];
+#pragma unroll
+                        for (int k = 0; k < V; ++k) y[k] = l == 0.f ? 0.f : __uint_as_float(v[i + k]) * inv;
+                        if (pieces) store_piece(dst + c + i, y);
+                        else
+#pragma unroll
+                            for (int k = 0; k < V; ++k) dst[c + i + k] = from_f32<T>(y[k]);
+                    }
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == MMA_WARP) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
+    }
+}
+
+template <int D, int NP, class T>
+int kp_launch(const Kv4Attend& a, cudaStream_t st) {
+    using C = KpCfg<D, NP>;
+    if (const int rc = allow_shared<kv4_prompt_kernel<D, NP, T>>(C::SMEM)) return rc;
+    const int64_t rows = (int64_t)a.c.most * a.group, tiles = (rows + C::ROWS - 1) / C::ROWS;
+    launch_chained(kv4_prompt_kernel<D, NP, T>, dim3((unsigned)(a.c.heads * a.c.sequences), (unsigned)tiles), C::THREADS, C::SMEM, st, a);
+    note_product(st);
+    return launch_status();
+}
+template <int NP, class T>
+int kp_launch_dim(const Kv4Attend& a, cudaStream_t st) {
+    return a.c.dim == 64 ? kp_launch<64, NP, T>(a, st) : kp_launch<128, NP, T>(a, st);
+}
+
+}  // namespace
+
+bool kv4_prompt_eligible(const Kv4Attend& a) {
+    const int64_t rows = (int64_t)a.c.most * a.group;
+    if ((a.c.dim != 64 && a.c.dim != 128) || rows < 128 || (rows + 127) / 128 > 65535 || (int64_t)a.c.heads * a.c.sequences > (1ll << 30)) return false;
+    return true;
+}
+
+int launch_kv4_prompt(const Kv4Attend& a, int dtype, cudaStream_t st) {
+    if (dtype == HBFP_F32) return kp_launch_dim<3, float>(a, st);
+    if (dtype == HBFP_BF16) return kp_launch_dim<1, __nv_bfloat16>(a, st);
+    return kp_launch_dim<2, __half>(a, st);
+}
+
+}  // namespace hbfp

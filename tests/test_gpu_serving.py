@@ -408,6 +408,53 @@ def test_attention_window(hb, dtype, window, n):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,heads,group,n", [(64, 1, 1, 128), (64, 2, 1, 300), (128, 1, 4, 64), (128, 2, 3, 100), (128, 1, 12, 33), (64, 1, 5, 257)])
+@pytest.mark.parametrize("window", [0, 1, 100])
+def test_attention_prompts(hb, dtype, D, heads, group, n, window):
+    """Rows enough for the kernel of many rows: prompts behind prefixes of no, few and many keys, and ones longer than their length."""
+    check_attention(hb, dtype, heads, group, D, 32, [n, n + 1, n + 63, n + 500, n - 7], [n] * 5, window=window)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [0.0, 3.0, -2.0, 1e-3])
+def test_attention_prompts_scales(hb, dtype, scale):
+    check_attention(hb, dtype, 1, 2, 64, 16, [500, 130], [130, 130], scale=scale)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_attention_prompts_ragged(hb, dtype):
+    """Prompts of 0 to 200 tokens in one call, queries and results slices of larger tensors, an invalid page among one sequence's."""
+    lengths, ns, D = [220, 7, 100, 2, 400, 0], [200, 0, 90, 5, 140, 2], 128
+    g = gen(19)
+    table, pages = pages_of(lengths, 16, g)
+    cache = fill(hb, g, pages, 2, 16, D)
+    rows = sum(ns)
+    q = normal(g, rows + 4, 9, D + 3).to(dtype)[:, 1:7, 2:D + 2]
+    big = torch.full((rows + 4, 8, D), 9.0, dtype=dtype, device="cuda")
+    out = big[:, 1:7]
+    starts = i32([0] + list(np.cumsum(ns)))
+    hb.kv4_attention(q, cache, table, i32(lengths), starts=starts, max_tokens=200, out=out)
+    ref, tol = attend_reference(q[:rows], cache, table, lengths, ns, D ** -0.5)
+    assert (out[:rows].double() - ref).abs().le(tol).all()
+    assert (out[rows:] == 9.0).all() and (big[:, 0] == 9.0).all() and (big[:, 7] == 9.0).all()
+    good = out.clone()
+    assert torch.equal(hb.kv4_attention(q, cache, table, i32(lengths), starts=starts, max_tokens=200)[:rows], good[:rows])
+    bad = table.clone()
+    bad[4, 3] = pages + 7                                                      # sixteen keys of the fifth sequence
+    assert hb.device_status() == 0
+    y = hb.kv4_attention(q, cache, bad, i32(lengths), starts=starts, max_tokens=200)
+    assert hb.device_status_rc() == (hb.ERR_INDEX, 1001)
+    assert torch.equal(y[:295], good[:295]) and torch.isfinite(y[:rows]).all() and not torch.equal(y[295:435], good[295:435])
+    free = list(range(48)) + list(range(64, 400))                              # the same as a sequence without those keys, for its last query
+    K, V = unpack(cache.k_mant, cache.k_exps), unpack(cache.v_mant, cache.v_exps)
+    at = torch.tensor(free, device="cuda")
+    ids = table[4].long()[at // 16]
+    k, v = K[ids, 0, at % 16], V[ids, 0, at % 16]
+    p = torch.softmax(q[434, 0].double() @ k.t() * D ** -0.5, -1)
+    assert (y[434, 0].double() - p @ v).abs().le(2 * tol[434, 0] + 1e-5).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_attention_ragged_tokens(hb, dtype):
     """Sequences of 0 to 50 new tokens, rows behind the last sequence's left as they were, first rows without a position."""
     lengths, ns = [30, 7, 100, 2, 400, 0], [3, 0, 50, 5, 1, 2]
