@@ -286,7 +286,7 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
             uint32_t s = 0, ph = 0;
             int it = 0;
             for (; it < steps; ++it) {
-                if (!mbar_wait(empty_bar + 8 * s, ph ^ 1, abort_flag, p.status, 171)) break;
+                if (!mbar_wait_soon(empty_bar + 8 * s, ph ^ 1, abort_flag, p.status, 171)) break;
                 mbar_expect_tx(full_bar + 8 * s, C::STAGE);
                 tma_load_2d(base + s * C::STAGE, &mapA, it * STAGE_K, m0, full_bar + 8 * s);
                 tma_load_2d(base + s * C::STAGE + TILE_M * STAGE_K, &mapB, it * STAGE_K, n0, full_bar + 8 * s);
@@ -295,14 +295,14 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
             // nothing of this CTA is in flight when it leaves
             for (int k = min(it, C::STAGES); k > 0; --k) {
                 if (s == 0) { s = C::STAGES - 1; ph ^= 1; } else { --s; }
-                mbar_wait(full_bar + 8 * s, ph, abort_flag, p.status, 172, false);
+                mbar_wait_soon(full_bar + 8 * s, ph, abort_flag, p.status, 172, false);
             }
         }
     } else if (warp == 1) {
         if (elect_one()) {
             uint32_t s = 0, ph = 0;
             for (int it = 0; it < steps; ++it) {
-                if (!mbar_wait(full_bar + 8 * s, ph, abort_flag, p.status, 173)) break;
+                if (!mbar_wait_soon(full_bar + 8 * s, ph, abort_flag, p.status, 173)) break;
                 tc_fence_after();
                 const uint64_t a = smem_desc_sw128(base + s * C::STAGE), b = smem_desc_sw128(base + s * C::STAGE + TILE_M * STAGE_K);
 #pragma unroll
@@ -311,7 +311,7 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 if (++s == C::STAGES) { s = 0; ph ^= 1; }
             }
             tc_commit(done_bar);
-            mbar_wait(done_bar, 0, abort_flag, p.status, 174, false);
+            mbar_wait_soon(done_bar, 0, abort_flag, p.status, 174, false);
         }
     } else {
         const int e = threadIdx.x - 64;
@@ -322,7 +322,7 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         const int quarter = warp & 3, row = m0 + quarter * 32 + lane;
         const float sa = row < p.M ? __ldg(p.sa + row) : 0.f;
         asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (mbar_wait_warp(done_bar, 0, abort_flag, p.status, 175)) {
+        if (mbar_wait_warp_soon(done_bar, 0, abort_flag, p.status, 175)) {
             tc_fence_after();
             const Int8Out out{p.tma_out ? &mapY : nullptr, p.y, p.ldy, p.M, p.N};
             unsigned char* box = sm + C::STAGES * C::STAGE + (warp - 2) * I8_BOX;
@@ -424,7 +424,7 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 pair_tile(w, tiles_m, tiles_n, tm, tn);
                 const int my_m = tm * 2 * TILE_M + (int)rank * TILE_M, my_n = tn * NT + (int)rank * (NT / 2);
                 for (int k = 0; k < steps; ++k, ++it) {
-                    if (!mbar_wait(empty_bar + 8 * s, ph ^ 1, abort_flag, p.status, 181)) { ok = false; break; }
+                    if (!mbar_wait_soon(empty_bar + 8 * s, ph ^ 1, abort_flag, p.status, 181)) { ok = false; break; }
                     if (rank == 0) mbar_expect_tx(full_bar + 8 * s, 2u * C::STAGE);
                     const uint32_t at = base + s * C::STAGE;
                     tma_load_2d_pair(at, &mapA, k * STAGE_K, my_m, leader_full + 8 * s, L2_EVICT_LAST);
@@ -436,7 +436,7 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
             if (rank == 0)
                 for (uint32_t back = min(it, (uint32_t)C::STAGES); back > 0; --back) {
                     if (s == 0) { s = C::STAGES - 1; ph ^= 1; } else { --s; }
-                    mbar_wait(full_bar + 8 * s, ph, abort_flag, p.status, 182, false);
+                    mbar_wait_soon(full_bar + 8 * s, ph, abort_flag, p.status, 182, false);
                 }
         }
     } else if (warp == 1) {
@@ -444,10 +444,10 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
             uint32_t s = 0, ph = 0, g = 0, gph = 1;
             bool ok = true;
             for (int w = cluster; ok && w < total; w += nclusters) {
-                if (!mbar_wait(tempty_bar + 8 * g, gph, abort_flag, p.status, 183)) break;
+                if (!mbar_wait_soon(tempty_bar + 8 * g, gph, abort_flag, p.status, 183)) break;
                 tc_fence_after();
                 for (int k = 0; k < steps; ++k) {
-                    if (!mbar_wait(full_bar + 8 * s, ph, abort_flag, p.status, 184)) { ok = false; break; }
+                    if (!mbar_wait_soon(full_bar + 8 * s, ph, abort_flag, p.status, 184)) { ok = false; break; }
                     tc_fence_after();
                     const uint64_t a = smem_desc_sw128(base + s * C::STAGE), b = smem_desc_sw128(base + s * C::STAGE + C::A_BYTES);
 #pragma unroll
@@ -459,7 +459,7 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 if (++g == C::GROUPS) { g = 0; gph ^= 1; }
             }
             tc_commit_pair(done_bar, 1);
-            mbar_wait(done_bar, 0, abort_flag, p.status, 185, false);
+            mbar_wait_soon(done_bar, 0, abort_flag, p.status, 185, false);
         }
     } else {
         const int e = warp - 2, quarter = warp & 3, half = e >> 2;
@@ -480,7 +480,7 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
             }
             const float sa = row < p.M ? __ldg(p.sa + row) : 0.f;
             __syncwarp();
-            if (!mbar_wait_warp_fast(tfull_bar + 8 * g, gph, abort_flag, p.status, 186)) break;
+            if (!mbar_wait_warp_soon(tfull_bar + 8 * g, gph, abort_flag, p.status, 186)) break;
             tc_fence_after();
             const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + g * NT + half * C::COLS;
             constexpr int CH = 32;

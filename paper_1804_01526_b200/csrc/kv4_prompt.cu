@@ -28,7 +28,10 @@ template <int D, int NP> struct KpCfg {
     static constexpr int QT = NP == 1 ? 2 : 1;                             // row tiles of a CTA
     static constexpr int ROWS = 128 * QT, HALVES = D / 64;
     static constexpr int TILE = HALVES * 16384;                            // 128 rows of D bfloat16, 128-byte columns swizzled
-    static constexpr int SOFT_WARPS = 4 * QT, FILL_WARPS = 4, THREADS = 32 * (SOFT_WARPS + FILL_WARPS + 1);
+    static constexpr int SOFT_WARPS = 4 * QT, FILL_WARPS = 4, THREADS = 32 * (SOFT_WARPS + FILL_WARPS + 4);      // the last four: one issues the MMAs
+    // registers by role, out of what the launch has (512 x 128 or 384 x 168)
+    static constexpr int REGS_SOFT = QT == 2 ? 168 : 232, REGS_FILL = QT == 2 ? 96 : 120, REGS_MMA = 56;
+    static_assert(32 * (SOFT_WARPS * REGS_SOFT + FILL_WARPS * REGS_FILL + 4 * REGS_MMA) <= THREADS * (QT == 2 ? 128 : 168) - 512, "register split");
     static constexpr int OFF_K = QT * NP * TILE, OFF_V = OFF_K + 2 * TILE, OFF_BAR = OFF_V + 2 * TILE;
     static constexpr int SMEM = 1024 + OFF_BAR + 512;
     static_assert(SMEM <= 232448, "shared memory");
@@ -61,6 +64,123 @@ __device__ __forceinline__ uint4 kp_unpack(uint32_t w, uint32_t scale, uint32_t 
     return make_uint4(ka_value(w, scale, offset), ka_value(w >> 4, scale, offset), ka_value(w >> 8, scale, offset), ka_value(w >> 12, scale, offset));
 }
 
+// What the rows of a warp see of 32 neighbouring keys: all of them, none, or (bits) some, each row its own. Only the keys around the diagonal, a
+// window's edge or a missing page are looked at one by one; with one code for all, the tests cost a whole tile as much as its arithmetic.
+enum Seen : int { SEEN_NONE, SEEN_SOME, SEEN_ALL };
+struct KpSight {
+    int first, last;         // limits of the warp's first and last row
+    int limit, window;       // this row's: key p is seen where p <= limit and limit - p < window
+    int missing;             // groups of sixteen of the tile that are not there
+    __device__ __forceinline__ Seen look(int pos, int c) const {
+        const int p = pos + c, gone = missing >> (c >> 4) & 3;
+        if (gone == 0 && p + 31 <= first && last - p < window) return SEEN_ALL;
+        if (gone == 3 || p > last || first - (p + 31) >= window) return SEEN_NONE;
+        return SEEN_SOME;
+    }
+    __device__ __forceinline__ uint32_t bits(int pos, int c) const {
+        const int p = pos + c, to = limit + 1 - p, from = limit - p - window + 1;        // columns [from, to)
+        uint32_t b = to <= 0 ? 0u : to >= 32 ? 0xFFFFFFFFu : (1u << to) - 1u;
+        b &= from <= 0 ? 0xFFFFFFFFu : from >= 32 ? 0u : 0xFFFFFFFFu << from;
+        const int gone = missing >> (c >> 4) & 3;
+        if (gone & 1) b &= 0xFFFF0000u;
+        if (gone & 2) b &= 0x0000FFFFu;
+        return b;
+    }
+};
+// The largest of a row's scores in tensor memory (columns sc ..), WHOLE: of all of the tile.
+__device__ __forceinline__ float kp_max32(const uint32_t (&x)[32], float top) {
+    float other = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+        asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(__uint_as_float(x[i])), "f"(__uint_as_float(x[i + 1])));
+        asm("max.f32 %0, %0, %1, %2;" : "+f"(other) : "f"(__uint_as_float(x[i + 2])), "f"(__uint_as_float(x[i + 3])));
+    }
+    return fmaxf(top, other);
+}
+__device__ __forceinline__ float kp_top(uint32_t sc, const KpSight& sight, int pos, bool whole) {
+    float top = -INFINITY;
+    if (whole) {
+        uint32_t v[2][32];
+        tc_ld32(sc, v[0]);
+#pragma unroll
+        for (int c = 0; c < KP_KEYS; c += 32) {
+            tc_wait_ld();
+            if (c + 32 < KP_KEYS) tc_ld32(sc + c + 32, v[(c / 32 + 1) & 1]);
+            top = kp_max32(v[c / 32 & 1], top);
+        }
+        return top;
+    }
+#pragma unroll 1
+    for (int c = 0; c < KP_KEYS; c += 32) {
+        const Seen how = sight.look(pos, c);
+        if (how == SEEN_NONE) continue;
+        uint32_t v[32];
+        tc_ld32(sc + c, v);
+        tc_wait_ld();
+        if (how == SEEN_SOME) {
+            const uint32_t bits = sight.bits(pos, c);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (!(bits >> i & 1)) v[i] = 0xFF800000u;
+        }
+        top = kp_max32(v, top);
+    }
+    return top;
+}
+// Its probabilities 2^(score * scale2 - m), as parts, to tensor memory (columns pc .., 64 a part); their sum is added to `sum`.
+template <int NP, bool SOME>
+__device__ __forceinline__ void kp_exp32(uint32_t sc, uint32_t pc, uint64_t k2, uint64_t m2, uint32_t bits, uint64_t (&sum)[2]) {
+    uint32_t v[32], x[NP][16];
+    tc_ld32(sc, v);
+    tc_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+        float e0, e1;
+        unpack2(ffma2(pack2(v[i], v[i + 1]), k2, m2), e0, e1);
+        e0 = ka_exp2(e0);
+        e1 = ka_exp2(e1);
+        if (SOME) {
+            if (!(bits >> i & 1)) e0 = 0.f;
+            if (!(bits >> (i + 1) & 1)) e1 = 0.f;
+        }
+        sum[i / 2 & 1] = fadd2(sum[i / 2 & 1], pack2(__float_as_uint(e0), __float_as_uint(e1)));
+        uint32_t parts[NP];
+        ka_parts<NP>(e0, e1, parts);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) x[p][i / 2] = parts[p];
+    }
+#pragma unroll
+    for (int p = 0; p < NP; ++p) tc_st16(pc + 64 * p, x[p]);
+}
+template <int NP>
+__device__ __forceinline__ float kp_probabilities(uint32_t sc, uint32_t pc, float scale2, float m, const KpSight& sight, int pos, bool whole) {
+    const uint64_t k2 = pack2(__float_as_uint(scale2), __float_as_uint(scale2)), m2 = pack2(__float_as_uint(-m), __float_as_uint(-m));
+    uint64_t sum[2] = {0ull, 0ull};
+    if (whole) {
+#pragma unroll
+        for (int c = 0; c < KP_KEYS; c += 32) kp_exp32<NP, false>(sc + c, pc + c / 2, k2, m2, 0u, sum);
+    } else {
+#pragma unroll 1
+        for (int c = 0; c < KP_KEYS; c += 32) {
+            const Seen how = sight.look(pos, c);
+            if (how == SEEN_NONE) {
+                uint32_t zero[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) zero[i] = 0u;
+#pragma unroll
+                for (int p = 0; p < NP; ++p) tc_st16(pc + 64 * p + c / 2, zero);
+            } else if (how == SEEN_SOME) {
+                kp_exp32<NP, true>(sc + c, pc + c / 2, k2, m2, sight.bits(pos, c), sum);
+            } else {
+                kp_exp32<NP, false>(sc + c, pc + c / 2, k2, m2, 0u, sum);
+            }
+        }
+    }
+    float s0, s1;
+    unpack2(fadd2(sum[0], sum[1]), s0, s1);
+    return s0 + s1;
+}
+
 template <int D, int NP, class T>
 __global__ void __launch_bounds__(KpCfg<D, NP>::THREADS, 1)
 kv4_prompt_kernel(const Kv4Attend a) {
@@ -69,7 +189,7 @@ kv4_prompt_kernel(const Kv4Attend a) {
     const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     unsigned char* sm = smem_dyn + (base - smem_u32(smem_dyn));
     const uint32_t bars = base + C::OFF_BAR;
-    const uint32_t kfull = bars, vfull = bars + 16, kempty = bars + 32, vempty = bars + 48, sfull = bars + 64, pfull = bars + 80, odone = bars + 96, done = bars + 112;
+    const uint32_t kfull = bars, vfull = bars + 16, kempty = bars + 32, vempty = bars + 48, sfull = bars + 64, pfull = bars + 80, odone = bars + 96, done = bars + 112, qfull = bars + 120;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + C::OFF_BAR + 128);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     volatile int* holes = reinterpret_cast<volatile int*>(tmem_slot + 4);        // [4 tiles][4 warps]: groups of sixteen keys that are not there
@@ -88,6 +208,7 @@ kv4_prompt_kernel(const Kv4Attend a) {
             mbar_init(odone + 8 * i, 1);
         }
         mbar_init(done, 1);
+        mbar_init(qfull, C::SOFT_WARPS);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -119,28 +240,8 @@ kv4_prompt_kernel(const Kv4Attend a) {
         }
         const float flip = a.scale2 < 0.f ? -1.f : 1.f, scale2 = fabsf(a.scale2);
 
-        // ---- the queries, in parts (a negative scale is a negative query)
-        const bool vec = ((reinterpret_cast<uintptr_t>(a.q) | (uintptr_t)((a.qs.token | a.qs.head) * (int64_t)sizeof(T))) & 15) == 0;
-        for (int i = threadIdx.x; i < C::ROWS * (D / 8); i += C::THREADS) {
-            const int r = i / (D / 8), c = i - r * (D / 8);
-            float e[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (r < rows) {
-                const int query = (r0 + r) / a.group, gh = r0 + r - query * a.group;
-                const T* src = reinterpret_cast<const T*>(a.q) + (seq.first + query) * a.qs.token + (h * a.group + gh) * a.qs.head + 8 * c;
-                if (vec) load8(src, e);
-                else load8_part(src, 8, e);
-            }
-            uint32_t x[4][NP];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) ka_parts<NP>(flip * e[2 * j], flip * e[2 * j + 1], x[j]);
-            unsigned char* at = sm + (r >> 7) * C::TILE + (c >> 3) * 16384 + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
-#pragma unroll
-            for (int p = 0; p < NP; ++p) *reinterpret_cast<uint4*>(at + p * C::TILE) = make_uint4(x[0][p], x[1][p], x[2][p], x[3][p]);
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncthreads();
-
         if (warp >= C::SOFT_WARPS && warp < MMA_WARP) {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_FILL));
             // ------------------------------------------------------------ unpacking: 32 keys of a tile per warp, a block of 32 values a lane and load
             constexpr int NBLK = D / 32, KPL = 32 / NBLK, LOADS = 32 / KPL;        // blocks of a row, keys of a load, loads of 32 keys
             const int w = warp - C::SOFT_WARPS, blk = (lane >> 3) % NBLK, sub = (lane & 7) + 8 * ((lane >> 3) / NBLK);
@@ -196,20 +297,21 @@ kv4_prompt_kernel(const Kv4Attend a) {
             for (int j = 0; j < most; ++j) {
                 const int s = j & 1;
                 const uint32_t ph = (uint32_t)((j >> 1) & 1) ^ 1u;
-                if (!mbar_wait_warp(kempty + 8 * s, ph, abort_flag, a.c.status, 191)) break;
+                if (!mbar_wait_warp_soon(kempty + 8 * s, ph, abort_flag, a.c.status, 191)) break;
                 if (lane == 0) holes[(j & 3) * 4 + w] = gone;
                 store(sm + C::OFF_K + s * C::TILE, kr, ke);
                 if (lane == 0) mbar_arrive(kfull + 8 * s);
                 find(j + 1);
                 load(a.c.k_mant, a.c.k_exps, kr, ke);
-                if (!mbar_wait_warp(vempty + 8 * s, ph, abort_flag, a.c.status, 192)) break;
+                if (!mbar_wait_warp_soon(vempty + 8 * s, ph, abort_flag, a.c.status, 192)) break;
                 store(sm + C::OFF_V + s * C::TILE, vr, ve);
                 if (lane == 0) mbar_arrive(vfull + 8 * s);
                 load(a.c.v_mant, a.c.v_exps, vr, ve);
             }
-        } else if (warp == MMA_WARP) {
+        } else if (warp >= MMA_WARP) {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_MMA));
             // ------------------------------------------------------------ MMAs
-            if (elect_one()) {
+            if (warp == MMA_WARP && elect_one()) {
                 auto scores = [&](int t, int j) {
                     const uint32_t d = tmem + C::S_COL + 128 * t, kt = base + C::OFF_K + (j & 1) * C::TILE;
 #pragma unroll
@@ -228,7 +330,7 @@ kv4_prompt_kernel(const Kv4Attend a) {
                         for (int i = 0; i < KP_KEYS / 16; ++i)
                             kp_mma_ts(d, pt + 64 * p + 8 * i, kp_desc_mn(vt + i * 2048), kp_idesc<D, true>(), j > 0 || p < NP - 1 || i > 0);
                 };
-                bool ok = most == 0 || mbar_wait(kfull, 0, abort_flag, a.c.status, 193);
+                bool ok = most == 0 || (mbar_wait_soon(qfull, 0, abort_flag, a.c.status, 189) && mbar_wait_soon(kfull, 0, abort_flag, a.c.status, 193));
                 if (ok && most > 0) {
                     tc_fence_after();
 #pragma unroll
@@ -241,12 +343,12 @@ kv4_prompt_kernel(const Kv4Attend a) {
                 }
                 for (int j = 0; ok && j < most; ++j) {
                     const int s = j & 1, s1 = (j + 1) & 1;
-                    if (!mbar_wait(vfull + 8 * s, (uint32_t)((j >> 1) & 1), abort_flag, a.c.status, 194)) { ok = false; break; }
-                    if (j + 1 < most && !mbar_wait(kfull + 8 * s1, (uint32_t)(((j + 1) >> 1) & 1), abort_flag, a.c.status, 195)) { ok = false; break; }
+                    if (!mbar_wait_soon(vfull + 8 * s, (uint32_t)((j >> 1) & 1), abort_flag, a.c.status, 194)) { ok = false; break; }
+                    if (j + 1 < most && !mbar_wait_soon(kfull + 8 * s1, (uint32_t)(((j + 1) >> 1) & 1), abort_flag, a.c.status, 195)) { ok = false; break; }
 #pragma unroll
                     for (int t = 0; t < C::QT; ++t) {
                         if (!ok || j >= n[t]) continue;
-                        if (!mbar_wait(pfull + 8 * t, (uint32_t)(j & 1), abort_flag, a.c.status, 196)) { ok = false; continue; }
+                        if (!mbar_wait_soon(pfull + 8 * t, (uint32_t)(j & 1), abort_flag, a.c.status, 196)) { ok = false; continue; }
                         tc_fence_after();
                         values(t, j);
                         if (j + 1 < n[t]) {
@@ -261,12 +363,47 @@ kv4_prompt_kernel(const Kv4Attend a) {
                     if (j + 1 < most) tc_commit(kempty + 8 * s1);
                 }
                 tc_commit(done);
-                mbar_wait(done, 0, abort_flag, a.c.status, 197, false);
+                mbar_wait_soon(done, 0, abort_flag, a.c.status, 197, false);
             }
         } else {
             // ------------------------------------------------------------ softmax: a row per thread
             const int t = warp >> 2, quarter = warp & 3, r = 128 * t + quarter * 32 + lane;
             const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), sc = lanes + C::S_COL + 128 * t, oc = lanes + C::O_COL + 128 * t, pc = lanes + C::P_COL + 128 * t;
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::REGS_SOFT));
+            // the queries first, in parts (a negative scale is a negative query); the loads of a round leave together
+            const bool vec = ((reinterpret_cast<uintptr_t>(a.q) | (uintptr_t)((a.qs.token | a.qs.head) * (int64_t)sizeof(T))) & 15) == 0;
+            constexpr int UNR = 8, UNITS = C::ROWS * (D / 8), ROUND = 32 * C::SOFT_WARPS;
+            for (int i0 = threadIdx.x; i0 < UNITS; i0 += UNR * ROUND) {
+                Eight<T> e[UNR];
+#pragma unroll
+                for (int k = 0; k < UNR; ++k) {
+                    const int i = i0 + k * ROUND, r = i / (D / 8), c = i - r * (D / 8);
+                    e[k].zero();
+                    if (r < rows) {
+                        const int query = (r0 + r) / a.group, gh = r0 + r - query * a.group;
+                        const T* src = reinterpret_cast<const T*>(a.q) + (seq.first + query) * a.qs.token + (h * a.group + gh) * a.qs.head + 8 * c;
+                        if (vec) e[k].load(src);
+                        else e[k].load_part(src, 8);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < UNR; ++k) {
+                    const int i = i0 + k * ROUND, r = i / (D / 8), c = i - r * (D / 8);
+                    float f[8];
+                    e[k].get(f);
+                    uint32_t x[4][NP];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) ka_parts<NP>(flip * f[2 * j], flip * f[2 * j + 1], x[j]);
+                    unsigned char* at = sm + (r >> 7) * C::TILE + (c >> 3) * 16384 + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) *reinterpret_cast<uint4*>(at + p * C::TILE) = make_uint4(x[0][p], x[1][p], x[2][p], x[3][p]);
+                }
+            }
+            static_assert(UNITS % (UNR * ROUND) == 0, "whole rounds");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(qfull);
+
             const int limit = first + (r0 + min(r, rows - 1)) / a.group, window = a.window ? a.window : 0x7fffffff;
             // rows of this warp: the first's limit and the last's, for a look at whole tiles
             const int limit0 = __reduce_min_sync(0xffffffffu, limit), limit1 = __reduce_max_sync(0xffffffffu, limit);
@@ -274,27 +411,13 @@ kv4_prompt_kernel(const Kv4Attend a) {
             bool ok = true;
             const int mine = t == 0 ? n[0] : n[C::QT - 1];
             for (int j = 0; j < mine; ++j) {
-                if (!mbar_wait_warp_fast(sfull + 8 * t, (uint32_t)(j & 1), abort_flag, a.c.status, 198)) { ok = false; break; }
+                if (!mbar_wait_warp_soon(sfull + 8 * t, (uint32_t)(j & 1), abort_flag, a.c.status, 198)) { ok = false; break; }
                 tc_fence_after();
                 const int pos = lo + j * KP_KEYS;
                 const int missing = holes[(j & 3) * 4] | holes[(j & 3) * 4 + 1] << 2 | holes[(j & 3) * 4 + 2] << 4 | holes[(j & 3) * 4 + 3] << 6;
+                const KpSight sight{limit0, limit1, limit, window, missing};
                 const bool whole = pos + KP_KEYS - 1 <= limit0 && limit1 - pos < window && missing == 0;
-                // columns [from, to) of the tile are seen by this row
-                const int to = min(limit + 1, hi) - pos, from = limit - pos - window + 1;
-                auto seen = [&](int c) { return c >= from && c < to && !(missing >> (c >> 4) & 1); };
-                float top = -INFINITY;
-#pragma unroll
-                for (int c = 0; c < KP_KEYS; c += 32) {
-                    uint32_t v[32];
-                    tc_ld32(sc + c, v);
-                    tc_wait_ld();
-                    if (!whole)
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (!seen(c + i)) v[i] = 0xFF800000u;
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(__uint_as_float(v[i])), "f"(__uint_as_float(v[i + 1])));
-                }
+                const float top = kp_top(sc, sight, pos, whole);
                 const float top2 = top == -INFINITY ? top : top * scale2;
                 const bool move = top2 > m + KP_SLACK || (m == -INFINITY && top2 != -INFINITY);
                 if (__any_sync(0xffffffffu, move)) {
@@ -315,42 +438,14 @@ kv4_prompt_kernel(const Kv4Attend a) {
                     }
                 }
                 const float m_use = m == -INFINITY ? 0.f : m;
-                const uint64_t k2 = pack2(__float_as_uint(scale2), __float_as_uint(scale2)), m2 = pack2(__float_as_uint(-m_use), __float_as_uint(-m_use));
-                uint64_t sum = 0ull;
-#pragma unroll
-                for (int c = 0; c < KP_KEYS; c += 32) {
-                    uint32_t v[32], x[NP][16];
-                    tc_ld32(sc + c, v);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        float e0, e1;
-                        unpack2(ffma2(pack2(v[i], v[i + 1]), k2, m2), e0, e1);
-                        if (!whole) {
-                            if (!seen(c + i)) e0 = -INFINITY;
-                            if (!seen(c + i + 1)) e1 = -INFINITY;
-                        }
-                        e0 = ka_exp2(e0);
-                        e1 = ka_exp2(e1);
-                        sum = fadd2(sum, pack2(__float_as_uint(e0), __float_as_uint(e1)));
-                        uint32_t parts[NP];
-                        ka_parts<NP>(e0, e1, parts);
-#pragma unroll
-                        for (int p = 0; p < NP; ++p) x[p][i / 2] = parts[p];
-                    }
-#pragma unroll
-                    for (int p = 0; p < NP; ++p) tc_st16(pc + 64 * p + c / 2, x[p]);
-                }
-                float s0, s1;
-                unpack2(sum, s0, s1);
-                l += s0 + s1;
+                l += kp_probabilities<NP>(sc, pc, scale2, m_use, sight, pos, whole);
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(pfull + 8 * t);
             }
             // ---- the row's result
-            if (ok && mine > 0) ok = mbar_wait_warp_fast(odone + 8 * t, 0, abort_flag, a.c.status, 199);
+            if (ok && mine > 0) ok = mbar_wait_warp_soon(odone + 8 * t, 0, abort_flag, a.c.status, 199);
             if (ok) {
                 tc_fence_after();
                 const float inv = l > 0.f ? __frcp_rn(l) : 0.f;            // a row that sees no key: zeros

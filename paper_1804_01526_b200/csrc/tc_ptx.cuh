@@ -102,6 +102,36 @@ __device__ __forceinline__ bool mbar_wait_warp_fast(uint32_t bar, uint32_t parit
         if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
     return mbar_wait_warp(bar, parity, abort_flag, status, code);
 }
+// Bounded waits that wake promptly however long they take: every look suspends the thread for the default time at most (one with the long hint
+// of mbar_wait wakes thousands of cycles late). For threads whose sub-partition has issue slots to spare.
+__device__ __forceinline__ bool mbar_wait_soon(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status, int code, bool heed_abort = true) {
+    if (mbar_try(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (;;) {
+        for (int i = 0; i < 64; ++i)
+            if (mbar_try(bar, parity)) return true;
+        if (heed_abort && *abort_flag) return false;
+        if (clock64() - t0 > WAIT_LIMIT_CYCLES) {
+            *abort_flag = 1;
+            atomicCAS(status, 0, code);
+            return false;
+        }
+    }
+}
+__device__ __forceinline__ bool mbar_wait_warp_soon(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status, int code) {
+    if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
+    const long long t0 = clock64();
+    for (;;) {
+        for (int i = 0; i < 64; ++i)
+            if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
+        const bool late = clock64() - t0 > WAIT_LIMIT_CYCLES;
+        if (__any_sync(0xffffffffu, late || *abort_flag != 0)) {
+            if (late) atomicCAS(status, 0, code);
+            *abort_flag = 1;
+            return false;
+        }
+    }
+}
 // Arrival of one lane of a converged warp, on a barrier of this CTA or (a cluster address) of any CTA of the cluster.
 __device__ __forceinline__ void mbar_arrive_elect(uint32_t bar) {
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\t@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar) : "memory");
