@@ -370,41 +370,49 @@ kv4_prompt_kernel(const Kv4Attend a) {
             const int t = warp >> 2, quarter = warp & 3, r = 128 * t + quarter * 32 + lane;
             const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), sc = lanes + C::S_COL + 128 * t, oc = lanes + C::O_COL + 128 * t, pc = lanes + C::P_COL + 128 * t;
             asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::REGS_SOFT));
-            // the queries first, in parts (a negative scale is a negative query); the loads of a round leave together
-            const bool vec = ((reinterpret_cast<uintptr_t>(a.q) | (uintptr_t)((a.qs.token | a.qs.head) * (int64_t)sizeof(T))) & 15) == 0;
-            constexpr int UNR = 8, UNITS = C::ROWS * (D / 8), ROUND = 32 * C::SOFT_WARPS;
-            for (int i0 = threadIdx.x; i0 < UNITS; i0 += UNR * ROUND) {
-                Eight<T> e[UNR];
-#pragma unroll
-                for (int k = 0; k < UNR; ++k) {
-                    const int i = i0 + k * ROUND, r = i / (D / 8), c = i - r * (D / 8);
-                    e[k].zero();
-                    if (r < rows) {
-                        const int query = (r0 + r) / a.group, gh = r0 + r - query * a.group;
-                        const T* src = reinterpret_cast<const T*>(a.q) + (seq.first + query) * a.qs.token + (h * a.group + gh) * a.qs.head + 8 * c;
-                        if (vec) e[k].load(src);
-                        else e[k].load_part(src, 8);
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k < UNR; ++k) {
-                    const int i = i0 + k * ROUND, r = i / (D / 8), c = i - r * (D / 8);
+            // The queries first, in parts (a negative scale is a negative query). A warp brings its own 32 rows: a lane knows where one of them is, all
+            // lanes load it. (A row looked up per 16 bytes: 6 us a CTA.)
+            const int own = r0 + r, own_query = own / a.group, own_head = h * a.group + own - own_query * a.group;
+            constexpr int CPR = D / 8, RPL = 32 / CPR;                      // pieces of eight values of a row, rows of a load
+            {
+                const bool vec = ((reinterpret_cast<uintptr_t>(a.q) | (uintptr_t)((a.qs.token | a.qs.head) * (int64_t)sizeof(T))) & 15) == 0;
+                const int64_t own_at = (seq.first + own_query) * a.qs.token + own_head * a.qs.head;
+                const int c = lane % CPR, sub = lane / CPR, row0 = 32 * quarter;
+                auto put = [&](int k, const Eight<T>& e) {
+                    const int line = row0 + k * RPL + sub;
                     float f[8];
-                    e[k].get(f);
+                    e.get(f);
                     uint32_t x[4][NP];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) ka_parts<NP>(flip * f[2 * j], flip * f[2 * j + 1], x[j]);
-                    unsigned char* at = sm + (r >> 7) * C::TILE + (c >> 3) * 16384 + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
+                    unsigned char* at = sm + t * C::TILE + (c >> 3) * 16384 + line * 128 + (((c & 7) ^ (line & 7)) << 4);
 #pragma unroll
                     for (int p = 0; p < NP; ++p) *reinterpret_cast<uint4*>(at + p * C::TILE) = make_uint4(x[0][p], x[1][p], x[2][p], x[3][p]);
+                };
+                constexpr int UNR = 8;
+#pragma unroll 1
+                for (int k0 = 0; k0 < 32 / RPL; k0 += UNR) {
+                    Eight<T> e[UNR];
+#pragma unroll
+                    for (int k = 0; k < UNR; ++k) {
+                        const int line = (k0 + k) * RPL + sub;
+                        const int64_t at = __shfl_sync(0xffffffffu, own_at, line);
+                        e[k].zero();
+                        if (128 * t + row0 + line < rows) {
+                            const T* src = reinterpret_cast<const T*>(a.q) + at + 8 * c;
+                            if (vec) e[k].load(src);
+                            else e[k].load_part(src, 8);
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < UNR; ++k) put(k0 + k, e[k]);
                 }
             }
-            static_assert(UNITS % (UNR * ROUND) == 0, "whole rounds");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(qfull);
 
-            const int limit = first + (r0 + min(r, rows - 1)) / a.group, window = a.window ? a.window : 0x7fffffff;
+            const int limit = r < rows ? first + own_query : first + (r0 + rows - 1) / a.group, window = a.window ? a.window : 0x7fffffff;
             // rows of this warp: the first's limit and the last's, for a look at whole tiles
             const int limit0 = __reduce_min_sync(0xffffffffu, limit), limit1 = __reduce_max_sync(0xffffffffu, limit);
             float m = -INFINITY, l = 0.f;
@@ -449,10 +457,10 @@ kv4_prompt_kernel(const Kv4Attend a) {
             if (ok) {
                 tc_fence_after();
                 const float inv = l > 0.f ? __frcp_rn(l) : 0.f;            // a row that sees no key: zeros
-                const int query = (r0 + r) / a.group, gh = r0 + r - query * a.group;
-                T* dst = reinterpret_cast<T*>(a.out) + (seq.first + query) * a.os.token + (h * a.group + gh) * a.os.head;
-                constexpr int V = 16 / sizeof(T);
-                const bool pieces = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)((a.os.token | a.os.head) * (int64_t)sizeof(T))) & 15) == 0;
+                // Through shared memory, in the place of the queries (all MMAs that read them have ended), out along the rows: 16 bytes of 32
+                // rows an instruction took 2 us.
+                constexpr int V = 16 / sizeof(T), PIECES = D / V, LINE = D * (int)sizeof(T), RPS = 32 / PIECES > 0 ? 32 / PIECES : 1;
+                unsigned char* area = sm + (t * 4 + quarter) * 32 * LINE;
 #pragma unroll
                 for (int c = 0; c < D; c += 32) {
                     uint32_t v[32];
@@ -463,16 +471,34 @@ kv4_prompt_kernel(const Kv4Attend a) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] = 0u;
                     }
-                    if (r >= rows) continue;
 #pragma unroll
                     for (int i = 0; i < 32; i += V) {
                         float y[V];
 #pragma unroll
                         for (int k = 0; k < V; ++k) y[k] = l == 0.f ? 0.f : __uint_as_float(v[i + k]) * inv;
-                        if (pieces) store_piece(dst + c + i, y);
-                        else
+                        store_piece(reinterpret_cast<T*>(area + lane * LINE + ((((c + i) / V) ^ (lane & 7)) << 4)), y);
+                    }
+                }
+                __syncwarp();
+                const bool vec = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)((a.os.token | a.os.head) * (int64_t)sizeof(T))) & 15) == 0;
+                const int64_t own_out = (seq.first + own_query) * a.os.token + own_head * a.os.head;
+                const int row0 = 128 * t + 32 * quarter;
+#pragma unroll 4
+                for (int k = 0; k < 32; k += RPS) {
+                    const int line = k + lane / PIECES % RPS;
+                    const int64_t at = __shfl_sync(0xffffffffu, own_out, line);
+                    if (row0 + line >= rows || (PIECES < 32 && lane / PIECES >= RPS)) continue;
 #pragma unroll
-                            for (int k = 0; k < V; ++k) dst[c + i + k] = from_f32<T>(y[k]);
+                    for (int c = lane % PIECES; c < PIECES; c += 32) {
+                        const uint4 y = *reinterpret_cast<const uint4*>(area + line * LINE + ((c ^ (line & 7)) << 4));
+                        T* dst = reinterpret_cast<T*>(a.out) + at + c * V;
+                        if (vec) {
+                            *reinterpret_cast<uint4*>(dst) = y;
+                        } else {
+                            const T* e = reinterpret_cast<const T*>(&y);
+#pragma unroll
+                            for (int i = 0; i < V; ++i) dst[i] = e[i];
+                        }
                     }
                 }
             }
