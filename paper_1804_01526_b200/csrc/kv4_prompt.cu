@@ -380,16 +380,21 @@ kv4_prompt_kernel(const Kv4Attend a) {
                 const int c = lane % CPR, sub = lane / CPR, row0 = 32 * quarter;
                 auto put = [&](int k, const Eight<T>& e) {
                     const int line = row0 + k * RPL + sub;
-                    float f[8];
-                    e.get(f);
-                    uint32_t x[4][NP];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) ka_parts<NP>(flip * f[2 * j], flip * f[2 * j + 1], x[j]);
                     unsigned char* at = sm + t * C::TILE + (c >> 3) * 16384 + line * 128 + (((c & 7) ^ (line & 7)) << 4);
+                    if constexpr (NP == 1) {
+                        const uint32_t sign = flip < 0.f ? 0x80008000u : 0u;
+                        *reinterpret_cast<uint4*>(at) = make_uint4(e.raw[0].x ^ sign, e.raw[0].y ^ sign, e.raw[0].z ^ sign, e.raw[0].w ^ sign);
+                    } else {
+                        float f[8];
+                        e.get(f);
+                        uint32_t x[4][NP];
 #pragma unroll
-                    for (int p = 0; p < NP; ++p) *reinterpret_cast<uint4*>(at + p * C::TILE) = make_uint4(x[0][p], x[1][p], x[2][p], x[3][p]);
+                        for (int j = 0; j < 4; ++j) ka_parts<NP>(flip * f[2 * j], flip * f[2 * j + 1], x[j]);
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) *reinterpret_cast<uint4*>(at + p * C::TILE) = make_uint4(x[0][p], x[1][p], x[2][p], x[3][p]);
+                    }
                 };
-                constexpr int UNR = 8;
+                constexpr int UNR = 32 / RPL < 16 ? 32 / RPL : 16;
 #pragma unroll 1
                 for (int k0 = 0; k0 < 32 / RPL; k0 += UNR) {
                     Eight<T> e[UNR];
