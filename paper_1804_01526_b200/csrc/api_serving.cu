@@ -26,7 +26,7 @@ int kv4_args(const hbfp_kv4_cache* c, const hbfp_kv4_batch* b, Kv4Args* a) {
     // grid extents, and positions, which are 32-bit numbers
     if (c->heads > 65535 || b->sequences > 65535 || b->tokens >= MOST || (int64_t)b->table_pages * c->page >= MOST) return HBFP_ERR_UNSUPPORTED;
     if (c->pages > 0 && (!c->k_mant || !c->k_exps || !c->v_mant || !c->v_exps)) return HBFP_ERR_INVALID_ARG;
-    if (!aligned(c->k_mant, 16) || !aligned(c->v_mant, 16)) return HBFP_ERR_ALIGNMENT;
+    if (!aligned(c->k_mant, 16) || !aligned(c->v_mant, 16) || !aligned(c->k_exps, 16) || !aligned(c->v_exps, 16)) return HBFP_ERR_ALIGNMENT;
     if (b->sequences > 0 && (!b->lengths || (b->table_pages > 0 && !b->table))) return HBFP_ERR_INVALID_ARG;
     if (!b->starts && (int64_t)b->sequences * b->max_tokens != b->tokens) return HBFP_ERR_INVALID_ARG;
     a->k_mant = c->k_mant;

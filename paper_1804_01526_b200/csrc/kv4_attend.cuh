@@ -13,7 +13,9 @@
 // products are exact and sums FP32. Softmax in base 2, running maximum and sum in FP32.
 //
 // Bound: reading the cache, dim / 2 + dim / 32 bytes per key and head and as much for values. Warps take 32 keys each in turn (16 of a
-// 256-wide head) and keep their own maximum and sum; the CTA joins them once at the end of its keys.
+// 256-wide head) and keep their own maximum and sum; the CTA joins them once at the end of its keys. Keys, values and exponents of a warp's
+// next chunks come by bulk copies into its own ring of shared memory (rows of a page and head are one run of memory), issued by one
+// lane, so that a warp has two chunks in flight without a register or an address for them.
 //
 // Split. Sequences differ in length and the host does not know the lengths, so a launch with long keys has as many CTAs as the GPU
 // holds at a time and each takes an equal share of all units (128 keys of one sequence, head and row tile), found by adding up the
@@ -60,10 +62,14 @@ template <int D> struct KaDim {
     static constexpr int UNIT = CH * KA_WARPS;             // keys of a CTA at a time
     static constexpr int STEPS = D / 16;                   // MMA steps along a key row
     static constexpr int KE = D == 128 || D == 64 ? 1 : 2; // exponents of a lane's key words
+    // a chunk in shared memory: keys, values, exponents of the keys, of the values
+    static constexpr int MANT = CH * D / 2, EXPS = CH * NB, CHUNK = 2 * (MANT + EXPS), STAGES = 3;
+    static_assert(MANT % 16 == 0 && EXPS % 16 == 0, "bulk copies");
 };
-template <int D, int NP, int NT> struct KaShared {                      // queries, then the warps' results in their place; maxima and sums
-    static constexpr int Q = NP * NT * KaDim<D>::STEPS * 256, OP = D + 4, O = KA_WARPS * 8 * NT * OP * 4;
-    static constexpr int ML = Q > O ? Q : O, BYTES = ML + KA_WARPS * 8 * NT * 8;
+template <int D, int NP, int NT> struct KaShared {                      // queries; the rings, then the warps' results in their place; maxima and sums; barriers
+    static constexpr int Q = NP * NT * KaDim<D>::STEPS * 256, OP = D + 4;
+    static constexpr int RING = KA_WARPS * KaDim<D>::STAGES * KaDim<D>::CHUNK, O = KA_WARPS * 8 * NT * OP * 4;
+    static constexpr int ML = Q + (RING > O ? RING : O), BAR = ML + KA_WARPS * 8 * NT * 8, BYTES = BAR + KA_WARPS * KaDim<D>::STAGES * 8 + 16;
 };
 
 __device__ __forceinline__ void ka_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint2 b) {
@@ -75,8 +81,8 @@ __device__ __forceinline__ uint32_t ka_transpose(uint32_t v) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
     return d;
 }
-// 2^s of two neighbours as a pair of bfloat16, and -136 * 2^s
-__device__ __forceinline__ uint32_t ka_scale(int s0, int s1) { return (uint32_t)((s0 + 127) | ((s1 + 127) << 16)) << 7; }
+// 2^s of two neighbours as a pair of bfloat16 ((s + 127) << 7 in each half), and -136 * 2^s
+__device__ __forceinline__ uint32_t ka_scale(int s0, int s1) { return (uint32_t)(s0 * 0x80 + (s1 * 0x800000 + 0x3F803F80)); }
 __device__ __forceinline__ uint32_t ka_offset(uint32_t scale) {
     uint32_t d;
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(scale), "r"(0xC308C308u));
@@ -106,33 +112,46 @@ __device__ __forceinline__ float ka_exp2(float x) {
 }
 
 template <int N>
-__device__ __forceinline__ void ka_load_words(const uint32_t* p, uint32_t (&w)[N]) {
+__device__ __forceinline__ void ka_load_words(uint32_t at, uint32_t (&w)[N]) {      // from shared memory
     if constexpr (N % 4 == 0) {
 #pragma unroll
-        for (int i = 0; i < N; i += 4) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4*>(p + i));
-            w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
-        }
+        for (int i = 0; i < N; i += 4)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i]), "=r"(w[i + 1]), "=r"(w[i + 2]), "=r"(w[i + 3]) : "r"(at + 4 * i));
     } else if constexpr (N == 2) {
-        const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-        w[0] = v.x; w[1] = v.y;
+        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = __ldg(p + i);
+        for (int i = 0; i < N; ++i) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[i]) : "r"(at + 4 * i));
     }
 }
+__device__ __forceinline__ int ka_load_byte(uint32_t at) {
+    int v;
+    asm volatile("ld.shared.s8 %0, [%1];" : "=r"(v) : "r"(at));
+    return v;
+}
+// size bytes of global memory to shared memory, counted on the barrier; all of them multiples of 16
+__device__ __forceinline__ void ka_copy(uint32_t dst, const void* src, uint32_t size, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(size), "r"(bar) : "memory");
+}
 
-// The keys [lo, hi) that the rows of a tile see, lo rounded down to a whole group of sixteen.
+// A warp's ring: its barriers and which phase each is in.
+struct KaRing {
+    uint32_t bars, phases;
+    volatile int* abort_flag;
+};
+
+// The keys [lo, hi) that the rows of a tile see, lo rounded down to a whole chunk.
 struct KaRange { int lo, hi; };
 
 // Row tile `tile` of (sequence b, head h): keys [lo, hi), result into `out` (slot < 0) or as a part.
 template <int D, int NP, int NT, class T>
-__device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq& seq, int h, int tile, KaRange range, int slot, unsigned char* sm) {
+__device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq& seq, int h, int tile, KaRange range, int slot, unsigned char* sm, KaRing& ring) {
     using C = KaDim<D>;
     constexpr int RT = 8 * NT, MT = C::CH / 16, TILES = 4 * C::VW;        // TILES: 16-row tiles of V^T
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int rows = min(RT, seq.n * a.group - tile * RT), r0 = tile * RT;
     uint2* qs = reinterpret_cast<uint2*>(sm);                             // [NP][NT][STEPS][32]
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // (copies follow where results were written)
     __syncthreads();                                                      // the tile before is through with shared memory
     for (int i = threadIdx.x; i < NT * C::STEPS * 32; i += KA_THREADS) {
         const int l = i & 31, step = (i >> 5) % C::STEPS, nt = (i >> 5) / C::STEPS, r = 8 * nt + (l >> 2);
@@ -171,61 +190,66 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
 #pragma unroll
         for (int c = 0; c < 2; ++c) { m[nt][c] = -INFINITY; l[nt][c] = 0.f; }
 
-    uint32_t kw[MT][2][C::NB], vw[MT][4][C::VW];
-    int8_t ke[MT][2][C::KE], ve[MT][4];
-    const int ke0 = (t * C::NB) >> 2;
-    // row of the cache's arrays where the sixteen keys from p on begin; -1: none of them are there
-    auto group_row = [&](int p) -> int64_t {
-        if (p >= range.hi) return -1;
-        const int64_t page = kv4_page(a.c, b, p >> a.c.shift);
-        return page < 0 ? -1 : ((page * a.c.heads + h) << a.c.shift) + (p & (a.c.page - 1));
+    // ---- the ring: lane 0 asks for the chunk at p (`gone`: which of its sixteens are not there), `id` is its page, looked up before
+    const uint32_t base = smem_u32(sm) + KaShared<D, NP, NT>::Q + warp * C::STAGES * C::CHUNK;
+    constexpr int GROUPS = C::CH / 16;
+    auto page_of = [&](int p) { return p < range.hi ? kv4_page(a.c, b, p >> a.c.shift) : (int64_t)-1; };
+    auto ask = [&](int p, int64_t id, int stage) {
+        const uint32_t at = base + stage * C::CHUNK, bar = ring.bars + 8 * stage;
+        const bool small = GROUPS == 2 && a.c.shift == 4;                  // a page of sixteen rows: the second half has its own
+        const int64_t id2 = small ? page_of(p + 16) : id;
+        const int keys1 = id < 0 ? 0 : small ? 16 : C::CH, keys2 = small && id2 >= 0 ? 16 : 0;
+        mbar_expect_tx(bar, (uint32_t)((keys1 + keys2) * (2 * (D / 2 + C::NB))));
+        auto copy = [&](int64_t page, int first, int keys) {
+            const int64_t row = ((page * a.c.heads + h) << a.c.shift) + ((p + first) & (a.c.page - 1));
+            ka_copy(at + first * (D / 2), a.c.k_mant + row * (D / 2), keys * (D / 2), bar);
+            ka_copy(at + C::MANT + first * (D / 2), a.c.v_mant + row * (D / 2), keys * (D / 2), bar);
+            ka_copy(at + 2 * C::MANT + first * C::NB, a.c.k_exps + row * C::NB, keys * C::NB, bar);
+            ka_copy(at + 2 * C::MANT + C::EXPS + first * C::NB, a.c.v_exps + row * C::NB, keys * C::NB, bar);
+        };
+        if (keys1) copy(id, 0, keys1);
+        if (keys2) copy(id2, 16, 16);
+        return (id < 0 ? (small ? 1 : 3) : 0) | (small && id2 < 0 ? 2 : 0);
     };
-    auto load_keys = [&](const int64_t (&row)[MT]) {
+    const int start = range.lo + warp * C::CH;
+    int64_t next_id = -1;
+    int gone = 0;                                                          // two bits a stage
+    if (lane == 0) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int hh = 0; hh < 2; ++hh) {
-                const int64_t at = max(row[i], (int64_t)0) + g + 8 * hh;
-                if (row[i] >= 0) {
-                    ka_load_words<C::NB>(reinterpret_cast<const uint32_t*>(a.c.k_mant) + at * (D / 8) + t * C::NB, kw[i][hh]);
-#pragma unroll
-                    for (int e = 0; e < C::KE; ++e) ke[i][hh][e] = __ldg(a.c.k_exps + at * C::NB + min(ke0 + e, C::NB - 1));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < C::NB; ++e) kw[i][hh][e] = 0;
-#pragma unroll
-                    for (int e = 0; e < C::KE; ++e) ke[i][hh][e] = 0;
-                }
-            }
-    };
-    auto load_values = [&](const int64_t (&row)[MT]) {
-        const int ve0 = (g * C::VW) >> 2;
-        const bool mine = D % 64 == 0 || g * C::VW < D / 8;
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t at = max(row[i], (int64_t)0) + 2 * t + (j & 1) + 8 * (j >> 1);
-                if (row[i] >= 0 && mine) {
-                    ka_load_words<C::VW>(reinterpret_cast<const uint32_t*>(a.c.v_mant) + at * (D / 8) + g * C::VW, vw[i][j]);
-                    ve[i][j] = __ldg(a.c.v_exps + at * C::NB + ve0);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < C::VW; ++e) vw[i][j][e] = 0;
-                    ve[i][j] = 0;
-                }
-            }
-    };
-
-    int64_t row[MT];
-    int pos = range.lo + warp * C::CH;
-    if (pos < range.hi) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i) row[i] = group_row(pos + 16 * i);
-        load_keys(row);
-        load_values(row);
+        for (int i = 0; i < C::STAGES - 1; ++i) {
+            const int p = start + i * C::UNIT;
+            if (p < range.hi) gone |= ask(p, page_of(p), i) << (2 * i);
+        }
+        next_id = page_of(start + (C::STAGES - 1) * C::UNIT);
     }
+    // row of this lane's keys g and g + 8 in the chunk: neighbours are swapped in every other pair, so that neither the keys' nor the values'
+    // accesses meet in a bank more than twice
+    const int gk = g ^ ((g >> 1) & 1), ke0 = (t * C::NB) >> 2, ve0 = (g * C::VW) >> 2;
+    const bool has_value = D % 64 == 0 || g * C::VW < D / 8;
+    int stage = 0;
+    bool ok = true;
+    int pos = start;
     for (; pos < range.hi; pos += C::UNIT) {
+        if (lane == 0) {
+            const int p = pos + (C::STAGES - 1) * C::UNIT, to = stage == 0 ? C::STAGES - 1 : stage - 1;
+            if (p < range.hi) {
+                gone = (gone & ~(3 << (2 * to))) | ask(p, next_id, to) << (2 * to);
+                next_id = page_of(p + C::UNIT);
+            }
+        }
+        const int missing = __shfl_sync(0xffffffffu, gone, 0) >> (2 * stage) & 3;
+        ok = mbar_wait_warp_soon(ring.bars + 8 * stage, ring.phases >> stage & 1, ring.abort_flag, a.c.status, 187);
+        if (!ok) break;
+        ring.phases ^= 1u << stage;
+        const uint32_t at = base + stage * C::CHUNK;
+        const bool whole = pos + C::CH <= range.hi && pos + C::CH - 1 <= first_limit && last_limit - pos < window && missing == 0;
+        // exponents of rows that are not whole's may be anything
+        auto exponent = [&](uint32_t where) { const int e = ka_load_byte(where); return whole ? e : kv4_exponent((int8_t)e); };
+        uint32_t kw[MT][2][C::NB];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int hh = 0; hh < 2; ++hh) ka_load_words<C::NB>(at + (16 * i + 8 * hh + gk) * (D / 2) + t * C::NB * 4, kw[i][hh]);
         // ---- S^T = K Q^T
         float s[MT][NT][4];
 #pragma unroll
@@ -241,7 +265,7 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
             for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
                 for (int e = 0; e < C::KE; ++e) {
-                    const int x = kv4_exponent(ke[i][hh][e]);
+                    const int x = exponent(at + 2 * C::MANT + (16 * i + 8 * hh + gk) * C::NB + min(ke0 + e, C::NB - 1));
                     sc[i][hh][e] = ka_scale(x, x);
                     of[i][hh][e] = ka_offset(sc[i][hh][e]);
                 }
@@ -277,15 +301,8 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
                     }
             }
         }
-        bool whole = pos + C::CH <= range.hi && pos + C::CH - 1 <= first_limit && last_limit - pos < window;
-#pragma unroll
-        for (int i = 0; i < MT; ++i) whole = whole && row[i] >= 0;
-        int64_t next[MT];
-#pragma unroll
-        for (int i = 0; i < MT; ++i) next[i] = group_row(pos + C::UNIT + 16 * i);
-        load_keys(next);
 
-        // ---- softmax in base 2: this lane holds keys g and g + 8 of every sixteen for its rows
+        // ---- softmax in base 2: this lane holds keys gk and gk + 8 of every sixteen for its rows
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -294,8 +311,8 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
                 for (int e = 0; e < 4; ++e) {
                     s[i][nt][e] *= a.scale2;
                     if (!whole) {
-                        const int p = pos + 16 * i + g + 8 * (e >> 1);
-                        if (row[i] < 0 || p >= range.hi || p > limit[nt][e & 1] || limit[nt][e & 1] - p >= window) s[i][nt][e] = -INFINITY;
+                        const int p = pos + 16 * i + gk + 8 * (e >> 1);
+                        if ((missing >> i & 1) || p >= range.hi || p > limit[nt][e & 1] || limit[nt][e & 1] - p >= window) s[i][nt][e] = -INFINITY;
                     }
                 }
         float top[NT][2];
@@ -344,12 +361,26 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
         // ---- O^T += V^T P^T
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            const uint32_t s01 = ka_scale(kv4_exponent(ve[i][0]), kv4_exponent(ve[i][1])), s23 = ka_scale(kv4_exponent(ve[i][2]), kv4_exponent(ve[i][3]));
+            uint32_t vw[4][C::VW];
+            int ve[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int r = 2 * t + (j & 1), key = 16 * i + (r ^ ((r >> 1) & 1)) + 8 * (j >> 1);
+                if (has_value) {
+                    ka_load_words<C::VW>(at + C::MANT + key * (D / 2) + g * C::VW * 4, vw[j]);
+                    ve[j] = exponent(at + 2 * C::MANT + C::EXPS + key * C::NB + ve0);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < C::VW; ++e) vw[j][e] = 0;
+                    ve[j] = 0;
+                }
+            }
+            const uint32_t s01 = ka_scale(ve[0], ve[1]), s23 = ka_scale(ve[2], ve[3]);
             const uint32_t o01 = ka_offset(s01), o23 = ka_offset(s23);
 #pragma unroll
             for (int w = 0; w < C::VW; ++w) {
-                const uint32_t x01 = __byte_perm(vw[i][0][w], vw[i][1][w], 0x5410), y01 = __byte_perm(vw[i][0][w], vw[i][1][w], 0x7632);
-                const uint32_t x23 = __byte_perm(vw[i][2][w], vw[i][3][w], 0x5410), y23 = __byte_perm(vw[i][2][w], vw[i][3][w], 0x7632);
+                const uint32_t x01 = __byte_perm(vw[0][w], vw[1][w], 0x5410), y01 = __byte_perm(vw[0][w], vw[1][w], 0x7632);
+                const uint32_t x23 = __byte_perm(vw[2][w], vw[3][w], 0x5410), y23 = __byte_perm(vw[2][w], vw[3][w], 0x7632);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const uint32_t f0 = ka_value(x01 >> (4 * e), s01, o01), f1 = ka_value(y01 >> (4 * e), s01, o01);
@@ -361,10 +392,12 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
                 }
             }
         }
-        load_values(next);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) row[i] = next[i];
+        __syncwarp();                                                      // all lanes are through with the chunk
+        stage = stage == C::STAGES - 1 ? 0 : stage + 1;
     }
+    // (given up: what was asked for lands before the CTA leaves)
+    if (!ok)
+        for (int i = 0; i < C::STAGES; ++i) mbar_wait_soon(ring.bars + 8 * i, ring.phases >> i & 1, ring.abort_flag, a.c.status, 188, false);
 
     // ---- the warps' parts joined
 #pragma unroll
@@ -373,9 +406,9 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
         for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], d);
-    __syncthreads();                                                      // all are through with the queries
+    __syncthreads();                                                      // all are through with their rings
     constexpr int OP = KaShared<D, NP, NT>::OP;
-    float* os = reinterpret_cast<float*>(sm);                             // [KA_WARPS][RT][OP]
+    float* os = reinterpret_cast<float*>(sm + KaShared<D, NP, NT>::Q);    // [KA_WARPS][RT][OP]
     float2* ml = reinterpret_cast<float2*>(sm + KaShared<D, NP, NT>::ML);      // [KA_WARPS][RT]
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -421,26 +454,43 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
     }
 }
 
+template <int D, int NP, int NT>
+__device__ __forceinline__ KaRing ka_ring(unsigned char* sm) {
+    using S = KaShared<D, NP, NT>;
+    constexpr int STAGES = KaDim<D>::STAGES;
+    volatile int* flag = reinterpret_cast<volatile int*>(sm + S::BAR + KA_WARPS * STAGES * 8);
+    const uint32_t bars = smem_u32(sm + S::BAR);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < KA_WARPS * STAGES; ++i) mbar_init(bars + 8 * i, 1);
+        *flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+    return KaRing{bars + (threadIdx.x >> 5) * STAGES * 8, 0u, flag};
+}
+
 __device__ __forceinline__ KaRange ka_range(const Kv4Attend& a, const Kv4Seq& s, int first_query, int last_query) {
     KaRange r;
     const int base = s.length - s.n;
     r.hi = max(0, min(s.length, base + last_query + 1));
-    r.lo = a.window ? max(0, base + first_query - a.window + 1) & ~15 : 0;
+    r.lo = a.window ? max(0, base + first_query - a.window + 1) & ~31 : 0;
     return r;
 }
 
 // A tile per CTA: short keys, or tiles enough.
 template <int D, int NP, int NT, class T>
-__global__ void __launch_bounds__(KA_THREADS)
+__global__ void __launch_bounds__(KA_THREADS, NT == 1 && D <= 128 ? 4 : 2)
 kv4_attend_kernel(const Kv4Attend a) {
-    extern __shared__ __align__(16) unsigned char sm[];
+    extern __shared__ __align__(128) unsigned char sm[];
+    KaRing ring = ka_ring<D, NP, NT>(sm);
     chain_start();
     const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x;
     const Kv4Seq s = kv4_seq(a.c, b);
     constexpr int RT = 8 * NT;
     if (tile * RT >= s.n * a.group) return;
     const int last = min((tile + 1) * RT, s.n * a.group) - 1;
-    ka_tile<D, NP, NT, T>(a, b, s, h, tile, ka_range(a, s, tile * RT / a.group, last / a.group), -1, sm);
+    ka_tile<D, NP, NT, T>(a, b, s, h, tile, ka_range(a, s, tile * RT / a.group, last / a.group), -1, sm, ring);
 }
 
 // The units of a sequence's tiles (all alike) and how many tiles it has.
@@ -480,10 +530,11 @@ __device__ __forceinline__ void ka_scan(const Kv4Attend& a, int& total, int& bef
 }
 
 template <int D, int NP, int NT, class T>
-__global__ void __launch_bounds__(KA_THREADS)
+__global__ void __launch_bounds__(KA_THREADS, NT == 1 && D <= 128 ? 4 : 2)
 kv4_attend_split_kernel(const Kv4Attend a) {
-    extern __shared__ __align__(16) unsigned char sm[];
+    extern __shared__ __align__(128) unsigned char sm[];
     __shared__ int found[2];
+    KaRing ring = ka_ring<D, NP, NT>(sm);
     chain_start();
     int total, before, b0, b1;
     ka_scan<D, NT, KA_WARPS>(a, total, before, b0, b1);
@@ -509,7 +560,7 @@ kv4_attend_split_kernel(const Kv4Attend a) {
             r.lo = all.lo + within * KaDim<D>::UNIT;
             r.hi = min(all.hi, r.lo + take * KaDim<D>::UNIT);
             const int slot = take == x.x ? -1 : 2 * cta + (within == 0);
-            ka_tile<D, NP, NT, T>(a, b, s, h, tile, r, slot, sm);
+            ka_tile<D, NP, NT, T>(a, b, s, h, tile, r, slot, sm, ring);
             at += take;
             u += take;
         }
