@@ -150,6 +150,7 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
     constexpr int RT = 8 * NT, MT = C::CH / 16, TILES = 4 * C::VW;        // TILES: 16-row tiles of V^T
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int rows = min(RT, seq.n * a.group - tile * RT), r0 = tile * RT;
+    const float flip = a.scale2 < 0.f ? -1.f : 1.f, scale2 = fmaxf(fabsf(a.scale2), 1e-37f);      // a negative scale is a negative query; 0 times an unseen -inf would be NaN
     uint2* qs = reinterpret_cast<uint2*>(sm);                             // [NP][NT][STEPS][32]
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // (copies follow where results were written)
     __syncthreads();                                                      // the tile before is through with shared memory
@@ -160,7 +161,7 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
             const int query = (r0 + r) / a.group, gh = (r0 + r) - query * a.group;
             const T* src = reinterpret_cast<const T*>(a.q) + (seq.first + query) * a.qs.token + (h * a.group + gh) * a.qs.head + ((l & 3) * C::NB + (step >> 1)) * 8 + 4 * (step & 1);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] = to_f32(src[j]);
+            for (int j = 0; j < 4; ++j) e[j] = flip * to_f32(src[j]);
         }
         uint32_t x[NP], y[NP];
         ka_parts<NP>(e[0], e[1], x);
@@ -190,38 +191,39 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
 #pragma unroll
         for (int c = 0; c < 2; ++c) { m[nt][c] = -INFINITY; l[nt][c] = 0.f; }
 
-    // ---- the ring: lane 0 asks for the chunk at p (`gone`: which of its sixteens are not there), `id` is its page, looked up before
+    // ---- the ring. Lanes 0 to 3 each ask for one of a chunk's arrays (keys, values, their exponents); every lane knows the page of the
+    // chunk after the last one asked for. gone: which sixteens of each stage's chunk are not there, two bits a stage.
     const uint32_t base = smem_u32(sm) + KaShared<D, NP, NT>::Q + warp * C::STAGES * C::CHUNK;
     constexpr int GROUPS = C::CH / 16;
-    auto page_of = [&](int p) { return p < range.hi ? kv4_page(a.c, b, p >> a.c.shift) : (int64_t)-1; };
-    auto ask = [&](int p, int64_t id, int stage) {
-        const uint32_t at = base + stage * C::CHUNK, bar = ring.bars + 8 * stage;
-        const bool small = GROUPS == 2 && a.c.shift == 4;                  // a page of sixteen rows: the second half has its own
-        const int64_t id2 = small ? page_of(p + 16) : id;
-        const int keys1 = id < 0 ? 0 : small ? 16 : C::CH, keys2 = small && id2 >= 0 ? 16 : 0;
-        mbar_expect_tx(bar, (uint32_t)((keys1 + keys2) * (2 * (D / 2 + C::NB))));
-        auto copy = [&](int64_t page, int first, int keys) {
-            const int64_t row = ((page * a.c.heads + h) << a.c.shift) + ((p + first) & (a.c.page - 1));
-            ka_copy(at + first * (D / 2), a.c.k_mant + row * (D / 2), keys * (D / 2), bar);
-            ka_copy(at + C::MANT + first * (D / 2), a.c.v_mant + row * (D / 2), keys * (D / 2), bar);
-            ka_copy(at + 2 * C::MANT + first * C::NB, a.c.k_exps + row * C::NB, keys * C::NB, bar);
-            ka_copy(at + 2 * C::MANT + C::EXPS + first * C::NB, a.c.v_exps + row * C::NB, keys * C::NB, bar);
-        };
-        if (keys1) copy(id, 0, keys1);
-        if (keys2) copy(id2, 16, 16);
+    const int mine = lane & 3;
+    const uint32_t line = mine < 2 ? D / 2 : C::NB, to_mine = (mine & 1) * (mine < 2 ? C::MANT : C::EXPS) + (mine < 2 ? 0 : 2 * C::MANT);
+    const int64_t page_bytes = ((int64_t)a.c.heads << a.c.shift) * line;
+    const char* const array = reinterpret_cast<const char*>(mine == 0 ? (const void*)a.c.k_mant : mine == 1 ? (const void*)a.c.v_mant : mine == 2 ? (const void*)a.c.k_exps
+                                                                                                                                       : (const void*)a.c.v_exps) +
+                              ((int64_t)h << a.c.shift) * line;
+    const bool small = GROUPS == 2 && a.c.shift == 4;                      // pages of sixteen rows: the second half of a chunk has its own
+    auto page_of = [&](int p) { return p < range.hi ? (int)kv4_page(a.c, b, p >> a.c.shift) : -1; };
+    auto ask = [&](int p, int id, int stage) {
+        const uint32_t at = base + stage * C::CHUNK + to_mine, bar = ring.bars + 8 * stage;
+        const uint32_t keys = id < 0 ? 0u : small ? 16u : (uint32_t)C::CH;
+        const int id2 = small ? page_of(p + 16) : -1;
+        if (lane == 0) mbar_expect_tx(bar, (keys + (id2 >= 0 ? 16u : 0u)) * (2 * (D / 2 + C::NB)));
+        __syncwarp();
+        if (lane < 4) {
+            const char* src = array + (uint32_t)(p & (a.c.page - 1)) * line;
+            if (id >= 0) ka_copy(at, src + id * page_bytes, keys * line, bar);
+            if (small && id2 >= 0) ka_copy(at + 16 * line, array + id2 * page_bytes, 16 * line, bar);
+        }
         return (id < 0 ? (small ? 1 : 3) : 0) | (small && id2 < 0 ? 2 : 0);
     };
     const int start = range.lo + warp * C::CH;
-    int64_t next_id = -1;
-    int gone = 0;                                                          // two bits a stage
-    if (lane == 0) {
+    int gone = 0;
 #pragma unroll
-        for (int i = 0; i < C::STAGES - 1; ++i) {
-            const int p = start + i * C::UNIT;
-            if (p < range.hi) gone |= ask(p, page_of(p), i) << (2 * i);
-        }
-        next_id = page_of(start + (C::STAGES - 1) * C::UNIT);
+    for (int i = 0; i < C::STAGES - 1; ++i) {
+        const int p = start + i * C::UNIT;
+        if (p < range.hi) gone |= ask(p, page_of(p), i) << (2 * i);
     }
+    int next_id = page_of(start + (C::STAGES - 1) * C::UNIT);
     // row of this lane's keys g and g + 8 in the chunk: neighbours are swapped in every other pair, so that neither the keys' nor the values'
     // accesses meet in a bank more than twice
     const int gk = g ^ ((g >> 1) & 1), ke0 = (t * C::NB) >> 2, ve0 = (g * C::VW) >> 2;
@@ -230,21 +232,30 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
     bool ok = true;
     int pos = start;
     for (; pos < range.hi; pos += C::UNIT) {
-        if (lane == 0) {
+        {
             const int p = pos + (C::STAGES - 1) * C::UNIT, to = stage == 0 ? C::STAGES - 1 : stage - 1;
             if (p < range.hi) {
                 gone = (gone & ~(3 << (2 * to))) | ask(p, next_id, to) << (2 * to);
                 next_id = page_of(p + C::UNIT);
             }
         }
-        const int missing = __shfl_sync(0xffffffffu, gone, 0) >> (2 * stage) & 3;
+        const int missing = gone >> (2 * stage) & 3;
         ok = mbar_wait_warp_soon(ring.bars + 8 * stage, ring.phases >> stage & 1, ring.abort_flag, a.c.status, 187);
         if (!ok) break;
         ring.phases ^= 1u << stage;
         const uint32_t at = base + stage * C::CHUNK;
         const bool whole = pos + C::CH <= range.hi && pos + C::CH - 1 <= first_limit && last_limit - pos < window && missing == 0;
-        // exponents of rows that are not whole's may be anything
-        auto exponent = [&](uint32_t where) { const int e = ka_load_byte(where); return whole ? e : kv4_exponent((int8_t)e); };
+        if (!whole) {
+            // rows that nobody appended may hold any exponent: brought into range, so that a probability of zero leaves nothing of them
+            for (int i = lane; i < 2 * C::EXPS / 4; i += 32) {
+                uint32_t e;
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(e) : "r"(at + 2 * C::MANT + 4 * i));
+                e = __vmins4(__vmaxs4(e, 0xC1C1C1C1u), (uint32_t)KV4_MAX_EXP * 0x01010101u);
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + 2 * C::MANT + 4 * i), "r"(e) : "memory");
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the next copy to this place comes after
+            __syncwarp();
+        }
         uint32_t kw[MT][2][C::NB];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -265,7 +276,7 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
             for (int hh = 0; hh < 2; ++hh)
 #pragma unroll
                 for (int e = 0; e < C::KE; ++e) {
-                    const int x = exponent(at + 2 * C::MANT + (16 * i + 8 * hh + gk) * C::NB + min(ke0 + e, C::NB - 1));
+                    const int x = ka_load_byte(at + 2 * C::MANT + (16 * i + 8 * hh + gk) * C::NB + min(ke0 + e, C::NB - 1));
                     sc[i][hh][e] = ka_scale(x, x);
                     of[i][hh][e] = ka_offset(sc[i][hh][e]);
                 }
@@ -303,18 +314,16 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
         }
 
         // ---- softmax in base 2: this lane holds keys gk and gk + 8 of every sixteen for its rows
+        if (!whole)
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+            for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[i][nt][e] *= a.scale2;
-                    if (!whole) {
+                    for (int e = 0; e < 4; ++e) {
                         const int p = pos + 16 * i + gk + 8 * (e >> 1);
                         if ((missing >> i & 1) || p >= range.hi || p > limit[nt][e & 1] || limit[nt][e & 1] - p >= window) s[i][nt][e] = -INFINITY;
                     }
-                }
         float top[NT][2];
         bool grows = false;
 #pragma unroll
@@ -324,7 +333,7 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
                 float x = fmaxf(s[0][nt][c], s[0][nt][c + 2]);
 #pragma unroll
                 for (int i = 1; i < MT; ++i) x = fmaxf(x, fmaxf(s[i][nt][c], s[i][nt][c + 2]));
-                top[nt][c] = x;
+                top[nt][c] = x = x * scale2;
                 grows |= x > m[nt][c];
             }
         if (__any_sync(0xffffffffu, grows)) {
@@ -348,7 +357,10 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
             const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                const float p0 = ka_exp2(s[i][nt][0] - m0), p1 = ka_exp2(s[i][nt][1] - m1), p2 = ka_exp2(s[i][nt][2] - m0), p3 = ka_exp2(s[i][nt][3] - m1);
+                float x0[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x0[e] = ka_exp2(__fmaf_rn(s[i][nt][e], scale2, e & 1 ? -m1 : -m0));
+                const float p0 = x0[0], p1 = x0[1], p2 = x0[2], p3 = x0[3];
                 l[nt][0] += p0 + p2;
                 l[nt][1] += p1 + p3;
                 uint32_t x[NP], y[NP];
@@ -368,7 +380,7 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
                 const int r = 2 * t + (j & 1), key = 16 * i + (r ^ ((r >> 1) & 1)) + 8 * (j >> 1);
                 if (has_value) {
                     ka_load_words<C::VW>(at + C::MANT + key * (D / 2) + g * C::VW * 4, vw[j]);
-                    ve[j] = exponent(at + 2 * C::MANT + C::EXPS + key * C::NB + ve0);
+                    ve[j] = ka_load_byte(at + 2 * C::MANT + C::EXPS + key * C::NB + ve0);
                 } else {
 #pragma unroll
                     for (int e = 0; e < C::VW; ++e) vw[j][e] = 0;
