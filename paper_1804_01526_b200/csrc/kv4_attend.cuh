@@ -134,6 +134,18 @@ __device__ __forceinline__ void ka_copy(uint32_t dst, const void* src, uint32_t 
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(size), "r"(bar) : "memory");
 }
 
+// From the shared memory of any CTA of the cluster.
+__device__ __forceinline__ float2 ka_shared2(uint32_t at) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ka_shared4(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+
 // A warp's ring: its barriers and which phase each is in.
 struct KaRing {
     uint32_t bars, phases;
@@ -143,9 +155,10 @@ struct KaRing {
 // The keys [lo, hi) that the rows of a tile see, lo rounded down to a whole chunk.
 struct KaRange { int lo, hi; };
 
-// Row tile `tile` of (sequence b, head h): keys [lo, hi), result into `out` (slot < 0) or as a part.
+// Row tile `tile` of (sequence b, head h): keys [lo, hi), result into `out` (slot < 0) or as a part. splits: the CTAs of a cluster have a share of the
+// tile's keys each and join them here.
 template <int D, int NP, int NT, class T>
-__device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq& seq, int h, int tile, KaRange range, int slot, unsigned char* sm, KaRing& ring) {
+__device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq& seq, int h, int tile, KaRange range, int slot, int splits, unsigned char* sm, KaRing& ring) {
     using C = KaDim<D>;
     constexpr int RT = 8 * NT, MT = C::CH / 16, TILES = 4 * C::VW;        // TILES: 16-row tiles of V^T
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -438,19 +451,29 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
             for (int c = 0; c < 2; ++c) ml[warp * RT + 8 * nt + 2 * t + c] = make_float2(m[nt][c], l[nt][c]);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < rows * (D / 4); i += KA_THREADS) {
+    if (splits > 1) cluster_barrier();
+    const int rank = splits > 1 ? (int)cluster_ctarank() : 0;
+    const uint32_t os_at = smem_u32(os), ml_at = smem_u32(ml);
+    for (int i = rank * KA_THREADS + threadIdx.x; i < rows * (D / 4); i += splits * KA_THREADS) {
         const int r = i / (D / 4), d = 4 * (i - r * (D / 4));
         float top = -INFINITY, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int sp = 0; sp < splits; ++sp) {
+            const uint32_t from = splits > 1 ? map_to_rank(ml_at, sp) : ml_at;
 #pragma unroll
-        for (int w = 0; w < KA_WARPS; ++w) top = fmaxf(top, ml[w * RT + r].x);
+            for (int w = 0; w < KA_WARPS; ++w) top = fmaxf(top, ka_shared2(from + (w * RT + r) * 8).x);
+        }
         if (top != -INFINITY)
+#pragma unroll 2
+            for (int sp = 0; sp < splits; ++sp) {
+                const uint32_t from = splits > 1 ? map_to_rank(ml_at, sp) : ml_at, of = splits > 1 ? map_to_rank(os_at, sp) : os_at;
 #pragma unroll
-            for (int w = 0; w < KA_WARPS; ++w) {
-                const float2 x = ml[w * RT + r];
-                const float f = ka_exp2(x.x - top);
-                const float4 y = *reinterpret_cast<const float4*>(os + (w * RT + r) * OP + d);
-                sum += f * x.y;
-                v[0] += f * y.x; v[1] += f * y.y; v[2] += f * y.z; v[3] += f * y.w;
+                for (int w = 0; w < KA_WARPS; ++w) {
+                    const float2 x = ka_shared2(from + (w * RT + r) * 8);
+                    const float f = ka_exp2(x.x - top);
+                    const float4 y = ka_shared4(of + ((w * RT + r) * OP + d) * 4);
+                    sum += f * x.y;
+                    v[0] += f * y.x; v[1] += f * y.y; v[2] += f * y.z; v[3] += f * y.w;
+                }
             }
         if (slot >= 0) {
             float* part = a.partial + ((int64_t)slot * RT + r) * D + d;
@@ -490,19 +513,23 @@ __device__ __forceinline__ KaRange ka_range(const Kv4Attend& a, const Kv4Seq& s,
     return r;
 }
 
-// A tile per CTA: short keys, or tiles enough.
+// A tile per CTA, or per cluster of `splits` CTAs: short keys, or tiles enough.
 template <int D, int NP, int NT, class T>
 __global__ void __launch_bounds__(KA_THREADS, NT == 1 && D <= 128 ? 4 : 2)
-kv4_attend_kernel(const Kv4Attend a) {
+kv4_attend_kernel(const Kv4Attend a, int splits) {
     extern __shared__ __align__(128) unsigned char sm[];
     KaRing ring = ka_ring<D, NP, NT>(sm);
     chain_start();
-    const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x;
+    const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x / splits, rank = blockIdx.x % splits;
     const Kv4Seq s = kv4_seq(a.c, b);
-    constexpr int RT = 8 * NT;
-    if (tile * RT >= s.n * a.group) return;
+    constexpr int RT = 8 * NT, UNIT = KaDim<D>::UNIT;
+    if (tile * RT >= s.n * a.group) return;                               // (all of a cluster alike)
     const int last = min((tile + 1) * RT, s.n * a.group) - 1;
-    ka_tile<D, NP, NT, T>(a, b, s, h, tile, ka_range(a, s, tile * RT / a.group, last / a.group), -1, sm, ring);
+    KaRange r = ka_range(a, s, tile * RT / a.group, last / a.group);
+    const int units = (max(0, r.hi - r.lo) + UNIT - 1) / UNIT, u0 = units * rank / splits, u1 = units * (rank + 1) / splits;
+    r = KaRange{r.lo + u0 * UNIT, min(r.hi, r.lo + u1 * UNIT)};
+    ka_tile<D, NP, NT, T>(a, b, s, h, tile, r, -1, splits, sm, ring);
+    if (splits > 1) cluster_barrier();                                    // nobody reads this CTA's results any more
 }
 
 // The units of a sequence's tiles (all alike) and how many tiles it has.
@@ -572,7 +599,7 @@ kv4_attend_split_kernel(const Kv4Attend a) {
             r.lo = all.lo + within * KaDim<D>::UNIT;
             r.hi = min(all.hi, r.lo + take * KaDim<D>::UNIT);
             const int slot = take == x.x ? -1 : 2 * cta + (within == 0);
-            ka_tile<D, NP, NT, T>(a, b, s, h, tile, r, slot, sm, ring);
+            ka_tile<D, NP, NT, T>(a, b, s, h, tile, r, slot, 1, sm, ring);
             at += take;
             u += take;
         }
@@ -613,23 +640,49 @@ kv4_join_kernel(const Kv4Attend a, int each) {
     if (c0 == c1) return;
     const int rows = min(RT, s.n * a.group - tile * RT), group = threadIdx.x / LANES, d = 4 * (threadIdx.x % LANES), lane = threadIdx.x & 31;
     const float2* ml = reinterpret_cast<const float2*>(a.partial + (int64_t)2 * a.ctas * RT * D);
+    auto place = [&](int c, int r) { return (int64_t)(2 * c + (c == c0)) * RT + r; };
+    auto add = [&](int c, int r, float top, float& sum, float4& v) {
+        const float2 y = ml[place(c, r)];
+        const float4 w = *reinterpret_cast<const float4*>(a.partial + place(c, r) * D + d);
+        const float f = ka_exp2(y.x - top);
+        sum += f * y.y;
+        v.x += f * w.x; v.y += f * w.y; v.z += f * w.z; v.w += f * w.w;
+    };
+    auto store = [&](int r, float sum, const float4& v) {
+        const float inv = sum > 0.f ? __frcp_rn(sum) : 0.f;
+        const int query = (tile * RT + r) / a.group, gh = tile * RT + r - query * a.group;
+        T* dst = reinterpret_cast<T*>(a.out) + (s.first + query) * a.os.token + (h * a.group + gh) * a.os.head + d;
+        dst[0] = from_f32<T>(v.x * inv);
+        dst[1] = from_f32<T>(v.y * inv);
+        dst[2] = from_f32<T>(v.z * inv);
+        dst[3] = from_f32<T>(v.w * inv);
+    };
+    if (c1 - c0 < 8) {
+        // few parts: a row per group
+        if (group < GROUPS)
+            for (int r = row0 + group; r < min(rows, row0 + each); r += GROUPS) {
+                float top = -INFINITY, sum = 0.f;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                for (int c = c0; c <= c1; ++c) top = fmaxf(top, ml[place(c, r)].x);
+                if (top != -INFINITY) {
+#pragma unroll 4
+                    for (int c = c0; c <= c1; ++c) add(c, r, top, sum, v);
+                }
+                store(r, sum, v);
+            }
+        return;
+    }
     for (int r = row0; r < min(rows, row0 + each); ++r) {
-        auto place = [&](int c) { return (int64_t)(2 * c + (c == c0)) * RT + r; };
         float top = -INFINITY;
-        for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, ml[place(c)].x);
+        for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, ml[place(c, r)].x);
 #pragma unroll
         for (int k = 1; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
         float sum = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         if (top != -INFINITY && group < GROUPS) {
 #pragma unroll 4
-            for (int c = c0 + group; c <= c1; c += GROUPS) {
-                const float2 y = ml[place(c)];
-                const float4 w = *reinterpret_cast<const float4*>(a.partial + place(c) * D + d);
-                const float f = ka_exp2(y.x - top);
-                sum += f * y.y;
-                v.x += f * w.x; v.y += f * w.y; v.z += f * w.z; v.w += f * w.w;
-            }
+            for (int c = c0 + group; c <= c1; c += GROUPS) add(c, r, top, sum, v);
         }
         __syncthreads();                                                  // the row before has been stored
         if (group < GROUPS) {
@@ -644,13 +697,7 @@ kv4_join_kernel(const Kv4Attend a, int each) {
                 sum += weights[k];
                 v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
             }
-            const float inv = sum > 0.f ? __frcp_rn(sum) : 0.f;
-            const int query = (tile * RT + r) / a.group, gh = tile * RT + r - query * a.group;
-            T* dst = reinterpret_cast<T*>(a.out) + (s.first + query) * a.os.token + (h * a.group + gh) * a.os.head + d;
-            dst[0] = from_f32<T>(v.x * inv);
-            dst[1] = from_f32<T>(v.y * inv);
-            dst[2] = from_f32<T>(v.z * inv);
-            dst[3] = from_f32<T>(v.w * inv);
+            store(r, sum, v);
         }
     }
 }
@@ -681,14 +728,17 @@ int ka_launch(Kv4Attend a, cudaStream_t st, size_t* bytes) {
     a.tiles = (int)(((int64_t)a.c.most * a.group + RT - 1) / RT);
     const int64_t items = (int64_t)a.tiles * a.c.heads * a.c.sequences, units = (keys + KaDim<D>::UNIT - 1) / KaDim<D>::UNIT;
     const dim3 grid((unsigned)a.tiles, (unsigned)a.c.heads, (unsigned)a.c.sequences);
-    // A launch more and the parts' way through memory pay where a tile is long and the tiles do not fill the GPU several times.
-    const bool split = units > 2 && items < 4 * (int64_t)ctas && items * units < (1ll << 30);
+    // Clusters share a tile's keys while that leaves a CTA two units and the GPU has room for twice the CTAs.
+    int splits = 1;
+    while (splits < 8 && units > 2 * splits && items * splits * 2 <= ctas) splits *= 2;
+    // A launch more and the parts' way through memory pay where what is left to a CTA is long and the tiles do not fill the GPU.
+    const bool split = units > 12 * splits && items * splits < 2 * (int64_t)ctas && items * units < (1ll << 30);
     if (bytes) {
         *bytes = split ? (size_t)2 * ctas * RT * (D + 2) * sizeof(float) : 0;
         return HBFP_OK;
     }
     if (!split) {
-        launch_chained(kv4_attend_kernel<D, NP, NT, T>, grid, KA_THREADS, SMEM, st, a);
+        launch_chained_clusters(kv4_attend_kernel<D, NP, NT, T>, splits, dim3(grid.x * splits, grid.y, grid.z), KA_THREADS, SMEM, st, true, a, splits);
         return launch_status();
     }
     a.ctas = ctas;
