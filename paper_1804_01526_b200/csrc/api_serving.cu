@@ -7,6 +7,10 @@ int64_t int8_pitch(int64_t k);
 int launch_int8_quantize(const void* x, int dtype, int64_t d0, int64_t d1, int64_t ld, int axis, int8_t* q, int64_t pitch, float* scale, cudaStream_t st);
 int launch_int8_gemm(int64_t M, int64_t N, int64_t K, const int8_t* a, int64_t lda, const float* sa, const int8_t* b, int64_t ldb, const float* sb,
                      const float* bias, void* y, int dtype, int64_t ldy, cudaStream_t st);
+// One to three tokens, converted by the product's launch (int8_few.cu).
+bool int8_few_eligible(int64_t M, int64_t K);
+int launch_int8_few(int64_t M, int64_t N, int64_t K, const void* a, int a_dtype, int64_t lda, const float* sa, const int8_t* w, int64_t ldw, const float* sw,
+                    const float* bias, void* y, int dtype, int64_t ldy, cudaStream_t st);
 int launch_kv4_append(const Kv4Args& a, int dtype, const void* k, Kv4Rows ks, const void* v, Kv4Rows vs, cudaStream_t st);
 int launch_kv4_read(const Kv4Args& a, int count, float* k, float* v, cudaStream_t st);
 
@@ -89,7 +93,7 @@ int hbfp_int8_quantize(const void* x, int dtype, int64_t d0, int64_t d1, int64_t
 int hbfp_int8_gemm_workspace(int64_t M, int64_t N, int64_t K, int a_dtype, size_t* bytes) {
     if (!bytes || M < 0 || N < 0 || K < 0 || (a_dtype != HBFP_I8 && !dtype_ok(a_dtype))) return HBFP_ERR_INVALID_ARG;
     if (K >= INT8_MOST_K || M >= MOST || N >= MOST) return HBFP_ERR_UNSUPPORTED;
-    *bytes = a_dtype == HBFP_I8 || M == 0 || N == 0 || K == 0 ? 0 : (size_t)(round_up(M * int8_pitch(K), 256) + 4 * M);
+    *bytes = a_dtype == HBFP_I8 || M == 0 || N == 0 || K == 0 || int8_few_eligible(M, K) ? 0 : (size_t)(round_up(M * int8_pitch(K), 256) + 4 * M);
     return HBFP_OK;
 }
 
@@ -108,7 +112,9 @@ int hbfp_int8_gemm(int64_t M, int64_t N, int64_t K, const void* a, int a_dtype, 
         if (a_dtype == HBFP_I8) {
             if (!a_scale) return HBFP_ERR_INVALID_ARG;
             if (lda % 16 != 0 || !aligned(a, 16)) return HBFP_ERR_ALIGNMENT;
-        } else {
+        }
+        if (int8_few_eligible(M, K)) return launch_int8_few(M, N, K, a, a_dtype, lda, a_scale, w, ldw, w_scale, bias, y, y_dtype, ldy, st);
+        if (a_dtype != HBFP_I8) {
             if (!workspace || workspace_bytes < need) return HBFP_ERR_WORKSPACE;
             if (!aligned(workspace, 256)) return HBFP_ERR_ALIGNMENT;
             const int64_t pitch = int8_pitch(K);

@@ -6,65 +6,12 @@
 // and rounded to the result's type once.
 #include <cuda.h>
 
-#include "tc_ptx.cuh"
-#include "types.cuh"
+#include "int8.cuh"
 
 namespace hbfp {
 namespace {
 
 // ------------------------------------------------------------------------------ conversion
-
-// The scale of a row from its largest |x|, given as a bit pattern (so that NaN is larger than infinity, and infinity than any number).
-__device__ __forceinline__ float scale_of(uint32_t amax_bits) { return __fdiv_rn(__uint_as_float(amax_bits), 127.0f); }
-
-// How a row's values are divided by its scale: q = rint(x * inv) where the quotient is clear of the border between two whole numbers, by
-// more than the error of x * inv (2^-23 of 127 at most). Next to a border (one value in 5000) the remainder x - q * s decides: one FMA, and
-// exact there, since it is a multiple of half an ulp of s and no more than s / 2 and a little; the approximate quotient misses the right whole
-// number by one at most.
-struct Divider {
-    float s, inv;
-    bool small;              // inv is no normal number: the division is binary64's
-    __device__ __forceinline__ explicit Divider(float scale) : s(scale), inv(0.f), small(false) {
-        if (!(s > 0.f) || s > 3.0e38f) s = 0.f;              // an all-zero row, or one that holds an infinity or NaN: q = 0
-        else if (s < 1.0e-37f) small = true;
-        else inv = __frcp_rn(s);
-    }
-    __device__ __forceinline__ int exactly(float x) const {
-        const float t = __fmaf_rn(x, inv, 12582912.0f);      // 1.5 * 2^23: rounds to the nearest whole number, halves to even
-        const float r = __fmaf_rn(12582912.0f - t, s, x);
-        int n = __float_as_int(t) - 0x4B400000;
-        const float twice = fabsf(r) + fabsf(r);
-        if (s > 0.f && (twice > s || (twice == s && (n & 1)))) n += r > 0.f ? 1 : -1;
-        return n;
-    }
-    // (a scale below 1e-37 is coarse: it may have been rounded down far)
-    __device__ __forceinline__ int coarsely(float x) const { return max(-127, min(127, (int)rint((double)x / (double)s))); }
-    __device__ __forceinline__ int operator()(float x) const { return small ? coarsely(x) : exactly(x); }
-    // Eight values as bytes (not where the scale is `small`).
-    __device__ __forceinline__ uint2 eight(const float (&x)[8]) const {
-        const uint64_t inv2 = pack2(__float_as_uint(inv), __float_as_uint(inv)), up = pack2(0x4B400000u, 0x4B400000u), minus = pack2(0xBF800000u, 0xBF800000u);
-        float far = 0.f;
-        uint32_t n[8];
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const uint64_t v = pack2(__float_as_uint(x[i]), __float_as_uint(x[i + 1]));
-            const uint64_t t = ffma2(v, inv2, up), off = ffma2(v, inv2, ffma2(t, minus, up));        // up - t = -q
-            float t0, t1, o0, o1;
-            unpack2(t, t0, t1);
-            unpack2(off, o0, o1);
-            n[i] = __float_as_uint(t0);
-            n[i + 1] = __float_as_uint(t1);
-            asm("max.f32 %0, %0, %1, %2;" : "+f"(far) : "f"(fabsf(o0)), "f"(fabsf(o1)));
-        }
-        if (!(far < 0.4999f)) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) n[i] = (uint32_t)exactly(x[i]);
-        }
-        // (the low byte of 1.5 * 2^23 + q is that of q)
-        return make_uint2(__byte_perm(__byte_perm(n[0], n[1], 0x0040), __byte_perm(n[2], n[3], 0x0040), 0x5410),
-                          __byte_perm(__byte_perm(n[4], n[5], 0x0040), __byte_perm(n[6], n[7], 0x0040), 0x5410));
-    }
-};
 
 // Rows of x [rows][k] to q [rows][pitch] (bytes beyond k zero) and scale [rows]. GROUP threads take a row (a warp needs no barrier); it stays
 // in their registers, in its own type, up to KEEP * 8 values each, longer rows are read again (from L2). Bound by reading x and writing q:
@@ -174,6 +121,7 @@ struct Int8Problem {
     int64_t ldy;
     int32_t* status;
     int tma_out;                     // the result has a tensor map
+    int a_rows, stages, off_boxes;   // int8_gemm_kernel
 };
 
 // The way of a finished tile out of a warp: 32 rows (lane = row) x 128 bytes of the result at a time, scaled, the bias added and rounded, in
@@ -200,16 +148,16 @@ __device__ __forceinline__ void int8_fill_box(unsigned char* box, int j0, const 
 #pragma unroll
         for (int i = 0; i < V; i += 4) {
             const float4 s = *reinterpret_cast<const float4*>(sb + j + i), b = *reinterpret_cast<const float4*>(bias + j + i);
-            o[i] = __fmaf_rn((float)v[j + i] * sa, s.x, b.x);
-            o[i + 1] = __fmaf_rn((float)v[j + i + 1] * sa, s.y, b.y);
-            o[i + 2] = __fmaf_rn((float)v[j + i + 2] * sa, s.z, b.z);
-            o[i + 3] = __fmaf_rn((float)v[j + i + 3] * sa, s.w, b.w);
+            o[i] = int8_result(v[j + i], sa, s.x, b.x);
+            o[i + 1] = int8_result(v[j + i + 1], sa, s.y, b.y);
+            o[i + 2] = int8_result(v[j + i + 2], sa, s.z, b.z);
+            o[i + 3] = int8_result(v[j + i + 3], sa, s.w, b.w);
         }
         store_piece(reinterpret_cast<T*>(line + ((((j0 + j) / V) ^ (lane & 7)) << 4)), o);
     }
 }
 // The box leaves; it may be filled again after int8_box_free.
-template <class T>
+template <class T, int COLS = 128 / (int)sizeof(T)>
 __device__ __forceinline__ void int8_send_box(const Int8Out& out, unsigned char* box, int row0, int col0) {
     const int lane = threadIdx.x & 31;
     if (out.map) {
@@ -223,7 +171,6 @@ __device__ __forceinline__ void int8_send_box(const Int8Out& out, unsigned char*
         return;
     }
     __syncwarp();
-    constexpr int COLS = 128 / sizeof(T);
     T* y = reinterpret_cast<T*>(out.y);
     const int rows = min(32, out.M - row0);
     for (int r = 0; r < rows; ++r)
@@ -239,33 +186,41 @@ __device__ __forceinline__ void int8_box_free() {
 }
 
 // One 128 x NT tile per CTA: TMA fills stages of 128 bytes of K, one thread issues the MMAs, four warps read the finished int32 sums
-// from tensor memory, scale them and store.
+// from tensor memory, scale them and store. For products of few tiles, which a narrow NT spreads over the SMs, and which are bound by the
+// latency of what is in flight: a stage holds only the tokens that there are (`a_rows`, a multiple of eight: the MMA's other rows are whatever lies
+// behind, and are not stored), so that 24 tokens and 32 channels have 150 KB on the way.
+// Two columns of 128 bytes of K a stage: a commit and a look at a barrier for eight MMAs (17 tokens x 4096 x 4096: one column 12.0 us, two 9.7, four 10.2).
+constexpr int I8_STAGES = 8, I8_COLUMNS = 2, I8_STAGE_BYTES = 160 * 1024;
 template <int NT>
 struct I8Cfg {
-    static constexpr int STAGE = (TILE_M + NT) * STAGE_K;
-    static constexpr int STAGES = 5;
-    static constexpr int SMEM = 1024 + STAGES * STAGE + 4 * I8_BOX + 1024 + 8 * NT;
     static constexpr int THREADS = 192;
+    static constexpr int SMEM = 1024 + I8_STAGE_BYTES + (TILE_M * STAGE_K) + 4 * I8_BOX + 1024 + 8 * NT;       // at most
+    static int stages(int a_rows) { const int n = I8_STAGE_BYTES / (I8_COLUMNS * (a_rows + NT) * STAGE_K); return n < I8_STAGES ? n : I8_STAGES; }
+    // (behind the last stage the MMA still reads what its rows would be)
+    static int tiles(int a_rows) { return stages(a_rows) * I8_COLUMNS * (a_rows + NT) * STAGE_K + (TILE_M - a_rows) * STAGE_K; }
+    static int smem(int a_rows) { return 1024 + tiles(a_rows) + 4 * I8_BOX + 1024 + 8 * NT; }
 };
 
 template <class T, int NT>
 __global__ void __launch_bounds__(I8Cfg<NT>::THREADS)
 int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB, const __grid_constant__ CUtensorMap mapY, const Int8Problem p) {
-    using C = I8Cfg<NT>;
     extern __shared__ unsigned char smem_dyn[];
     const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
     unsigned char* sm = smem_dyn + (base - smem_u32(smem_dyn));
-    constexpr int BARS = C::STAGES * C::STAGE + 4 * I8_BOX;
-    const uint32_t full_bar = base + BARS, empty_bar = full_bar + 8 * C::STAGES, done_bar = empty_bar + 8 * C::STAGES;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(sm + BARS + 16 * C::STAGES + 8);
+    // [stages][NT channels, tokens], boxes on their way out, barriers, [NT] channel scales and [NT] biases
+    const int stages = p.stages;
+    const uint32_t column = (uint32_t)(p.a_rows + NT) * STAGE_K, stage = I8_COLUMNS * column;
+    unsigned char* boxes = sm + p.off_boxes;
+    const uint32_t full_bar = base + p.off_boxes + 4 * I8_BOX, empty_bar = full_bar + 8 * I8_STAGES, done_bar = empty_bar + 8 * I8_STAGES;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(boxes + 4 * I8_BOX + 16 * I8_STAGES + 8);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    float* cols = reinterpret_cast<float*>(sm + BARS + 1024);         // [NT] channel scales, [NT] biases
+    float* cols = reinterpret_cast<float*>(boxes + 4 * I8_BOX + 1024);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int m0 = blockIdx.y * TILE_M, n0 = blockIdx.x * NT;
-    const int steps = (p.K + STAGE_K - 1) / STAGE_K;
+    const int steps = (p.K + I8_COLUMNS * STAGE_K - 1) / (I8_COLUMNS * STAGE_K);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < C::STAGES; ++s) { mbar_init(full_bar + 8 * s, 1); mbar_init(empty_bar + 8 * s, 1); }
+        for (int s = 0; s < stages; ++s) { mbar_init(full_bar + 8 * s, 1); mbar_init(empty_bar + 8 * s, 1); }
         mbar_init(done_bar, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -287,14 +242,17 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
             int it = 0;
             for (; it < steps; ++it) {
                 if (!mbar_wait_soon(empty_bar + 8 * s, ph ^ 1, abort_flag, p.status, 171)) break;
-                mbar_expect_tx(full_bar + 8 * s, C::STAGE);
-                tma_load_2d(base + s * C::STAGE, &mapA, it * STAGE_K, m0, full_bar + 8 * s);
-                tma_load_2d(base + s * C::STAGE + TILE_M * STAGE_K, &mapB, it * STAGE_K, n0, full_bar + 8 * s);
-                if (++s == C::STAGES) { s = 0; ph ^= 1; }
+                mbar_expect_tx(full_bar + 8 * s, stage);
+#pragma unroll
+                for (int c = 0; c < I8_COLUMNS; ++c) {                        // (a column behind K is zeros)
+                    tma_load_2d(base + s * stage + c * column, &mapB, (I8_COLUMNS * it + c) * STAGE_K, n0, full_bar + 8 * s);
+                    tma_load_2d(base + s * stage + c * column + NT * STAGE_K, &mapA, (I8_COLUMNS * it + c) * STAGE_K, m0, full_bar + 8 * s);
+                }
+                if (++s == stages) { s = 0; ph ^= 1; }
             }
             // nothing of this CTA is in flight when it leaves
-            for (int k = min(it, C::STAGES); k > 0; --k) {
-                if (s == 0) { s = C::STAGES - 1; ph ^= 1; } else { --s; }
+            for (int k = min(it, stages); k > 0; --k) {
+                if (s == 0) { s = stages - 1; ph ^= 1; } else { --s; }
                 mbar_wait_soon(full_bar + 8 * s, ph, abort_flag, p.status, 172, false);
             }
         }
@@ -304,11 +262,14 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
             for (int it = 0; it < steps; ++it) {
                 if (!mbar_wait_soon(full_bar + 8 * s, ph, abort_flag, p.status, 173)) break;
                 tc_fence_after();
-                const uint64_t a = smem_desc_sw128(base + s * C::STAGE), b = smem_desc_sw128(base + s * C::STAGE + TILE_M * STAGE_K);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) tc_mma_i8(tmem_base, a + 2 * q, b + 2 * q, idesc_i8<NT>(), it > 0 || q > 0);
+                for (int c = 0; c < I8_COLUMNS; ++c) {
+                    const uint64_t b = smem_desc_sw128(base + s * stage + c * column), a = smem_desc_sw128(base + s * stage + c * column + NT * STAGE_K);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) tc_mma_i8(tmem_base, a + 2 * q, b + 2 * q, idesc_i8<NT>(), it > 0 || c > 0 || q > 0);
+                }
                 tc_commit(empty_bar + 8 * s);
-                if (++s == C::STAGES) { s = 0; ph ^= 1; }
+                if (++s == stages) { s = 0; ph ^= 1; }
             }
             tc_commit(done_bar);
             mbar_wait_soon(done_bar, 0, abort_flag, p.status, 174, false);
@@ -324,9 +285,9 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         asm volatile("bar.sync 1, 128;" ::: "memory");
         if (mbar_wait_warp_soon(done_bar, 0, abort_flag, p.status, 175)) {
             tc_fence_after();
-            const Int8Out out{p.tma_out ? &mapY : nullptr, p.y, p.ldy, p.M, p.N};
-            unsigned char* box = sm + C::STAGES * C::STAGE + (warp - 2) * I8_BOX;
-            constexpr int BOX = 128 / sizeof(T);
+            constexpr int BOX = NT < 128 / (int)sizeof(T) ? NT : 128 / (int)sizeof(T);       // 32 columns of 16 bits fill half of a box: copied out
+            const Int8Out out{p.tma_out && BOX * sizeof(T) == 128 ? &mapY : nullptr, p.y, p.ldy, p.M, p.N};
+            unsigned char* box = boxes + (warp - 2) * I8_BOX;
 #pragma unroll
             for (int c = 0; c < NT; c += 32) {
                 int v[32];
@@ -334,7 +295,7 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 tc_wait_ld();
                 if (c % BOX == 0) int8_box_free();
                 int8_fill_box<T>(box, c % BOX, v, sa, cols + c, cols + NT + c);
-                if ((c + 32) % BOX == 0) int8_send_box<T>(out, box, m0 + quarter * 32, n0 + c + 32 - BOX);
+                if ((c + 32) % BOX == 0) int8_send_box<T, BOX>(out, box, m0 + quarter * 32, n0 + c + 32 - BOX);
             }
             asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
         }
@@ -591,6 +552,23 @@ int launch_pair(Int8Problem p, const int8_t* a, int64_t lda, const int8_t* b, in
 // Enough 256 x 128 tiles to give every pair of SMs one.
 bool pair_eligible(int64_t M, int64_t N) { return M > 128 && (M + 255) / 256 * ((N + 127) / 128) >= 74; }
 
+template <class T, int NT>
+int launch_tiles(Int8Problem p, const int8_t* a, int64_t lda, const int8_t* b, int64_t ldb, cudaStream_t st) {
+    using C = I8Cfg<NT>;
+    p.a_rows = p.M < TILE_M ? (p.M + 7) / 8 * 8 : TILE_M;
+    p.stages = C::stages(p.a_rows);
+    p.off_boxes = C::tiles(p.a_rows);
+    CUtensorMap mA, mB, mY;
+    int rc = make_map(&mA, a, p.K, p.M, lda, STAGE_K, p.a_rows, true);
+    if (!rc) rc = make_map(&mB, b, p.K, p.N, ldb, STAGE_K, NT, true);
+    if (!rc) rc = map_result<T>(p, &mY);
+    if (!rc) rc = allow_shared<int8_gemm_kernel<T, NT>>(C::SMEM);
+    if (rc) return rc;
+    launch_chained(int8_gemm_kernel<T, NT>, dim3((p.N + NT - 1) / NT, (p.M + TILE_M - 1) / TILE_M), C::THREADS, C::smem(p.a_rows), st, mA, mB, mY, p);
+    note_product(st);
+    return launch_status();
+}
+
 template <class T>
 int product(Int8Problem p, const int8_t* a, int64_t lda, const int8_t* b, int64_t ldb, cudaStream_t st) {
     if (p.K == 0) {
@@ -605,16 +583,11 @@ int product(Int8Problem p, const int8_t* a, int64_t lda, const int8_t* b, int64_
         if ((halves + 73) / 74 * 6 < (tiles + 73) / 74 * 10) return launch_pair<T, 128>(p, a, lda, b, ldb, st);
         return launch_pair<T, 256>(p, a, lda, b, ldb, st);
     }
-    constexpr int NT = 128;
-    CUtensorMap mA, mB, mY;
-    int rc = make_map(&mA, a, p.K, p.M, lda, STAGE_K, TILE_M, true);
-    if (!rc) rc = make_map(&mB, b, p.K, p.N, ldb, STAGE_K, NT, true);
-    if (!rc) rc = map_result<T>(p, &mY);
-    if (!rc) rc = allow_shared<int8_gemm_kernel<T, NT>>(I8Cfg<NT>::SMEM);
-    if (rc) return rc;
-    launch_chained(int8_gemm_kernel<T, NT>, dim3((p.N + NT - 1) / NT, (p.M + TILE_M - 1) / TILE_M), I8Cfg<NT>::THREADS, I8Cfg<NT>::SMEM, st, mA, mB, mY, p);
-    note_product(st);
-    return launch_status();
+    // channels of a tile: as many as leave the SMs a tile each
+    const int64_t tiles_m = (p.M + TILE_M - 1) / TILE_M;
+    if (tiles_m * ((p.N + 127) / 128) >= 100) return launch_tiles<T, 128>(p, a, lda, b, ldb, st);
+    if (tiles_m * ((p.N + 63) / 64) >= 100) return launch_tiles<T, 64>(p, a, lda, b, ldb, st);
+    return launch_tiles<T, 32>(p, a, lda, b, ldb, st);
 }
 
 }  // namespace
@@ -629,7 +602,7 @@ int launch_int8_quantize(const void* x, int dtype, int64_t d0, int64_t d1, int64
 
 int launch_int8_gemm(int64_t M, int64_t N, int64_t K, const int8_t* a, int64_t lda, const float* sa, const int8_t* b, int64_t ldb, const float* sb,
                      const float* bias, void* y, int dtype, int64_t ldy, cudaStream_t st) {
-    Int8Problem p{(int)M, (int)N, (int)K, sa, sb, bias, y, ldy, device_status_word(), 0};
+    Int8Problem p{(int)M, (int)N, (int)K, sa, sb, bias, y, ldy, device_status_word(), 0, 0, 0, 0};
     if (!p.status) return HBFP_ERR_CUDA;
     if (dtype == HBFP_F32) return product<float>(p, a, lda, b, ldb, st);
     if (dtype == HBFP_BF16) return product<__nv_bfloat16>(p, a, lda, b, ldb, st);

@@ -125,6 +125,12 @@ struct Eight {
     }
 };
 
+// Four neighbouring elements; p must be aligned to four of them.
+__device__ __forceinline__ void store_four(float* p, const float (&v)[4]) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+template <class T>
+__device__ __forceinline__ void store_four(T* p, const float (&v)[4]) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_pair(v[0], v[1], p), pack_pair(v[2], v[3], p));
+}
 // Sixteen bytes; p must be 16-byte aligned.
 __device__ __forceinline__ void store_piece(float* p, const float (&v)[4]) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
 template <class T>

@@ -65,9 +65,9 @@ def test_int8_gemm_refusals(hb):
     for bad in (dict(M=-1), dict(K=-1), dict(ta=4), dict(ty=3), dict(ldy=7), dict(lda=19), dict(ldw=16), dict(a=None), dict(w=None), dict(sw=None), dict(y=None),
                 dict(ta=3, lda=32)):
         assert call(**bad) == hb.ERR_INVALID_ARG, bad
-    for bad in (dict(ldw=24), dict(w=P + 4), dict(ta=3, lda=24, sa=P), dict(ta=3, lda=32, sa=P, a=P + 1), dict(ws=P + 16)):
+    for bad in (dict(ldw=24), dict(w=P + 4), dict(ta=3, lda=24, sa=P), dict(ta=3, lda=32, sa=P, a=P + 1), dict(M=4000, ws=P + 16)):
         assert call(**bad) == hb.ERR_ALIGNMENT, bad
-    assert call(ws=None) == hb.ERR_WORKSPACE and call(bytes=16) == hb.ERR_WORKSPACE
+    assert call(M=4000, ws=None) == hb.ERR_WORKSPACE and call(M=4000, bytes=16) == hb.ERR_WORKSPACE
     for bad in (dict(K=131072, lda=131072, ldw=131072), dict(M=1 << 30), dict(N=1 << 30, ldy=1 << 30)):      # the sum has to fit int32
         assert call(**bad) == hb.ERR_UNSUPPORTED, bad
     assert call(M=0) == hb.OK and call(N=0, ldy=0) == hb.OK
