@@ -460,7 +460,7 @@ HBFP_API int hbfp_kv4_append(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* 
                              int64_t k_head, const void* v, int64_t v_token, int64_t v_head, void* stream);
 
 /* FP32 values of the last `count` positions of every sequence, k and v [sequences*count][heads][dim], zeros where
- * a position is negative (batch: table and lengths only). */
+ * a position is negative (batch: table and lengths only). k and v must be 32-byte aligned. */
 HBFP_API int hbfp_kv4_read(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int32_t count, float* k, float* v, void* stream);
 
 /* out[row][head] = sum_j p_j v_j with p = softmax_j(scale * q[row][head] . k_j) over the positions j <= own position

@@ -151,7 +151,7 @@ int hbfp_kv4_read(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int3
     if (const int rc = kv4_args(cache, &all, &a)) return rc;
     if (a.tokens == 0) return HBFP_OK;
     if (!k || !v) return HBFP_ERR_INVALID_ARG;
-    if (!aligned(k, 16) || !aligned(v, 16)) return HBFP_ERR_ALIGNMENT;
+    if (!aligned(k, 32) || !aligned(v, 32)) return HBFP_ERR_ALIGNMENT;
     a.status = device_status_word();
     if (!a.status) return HBFP_ERR_CUDA;
     return launch_kv4_read(a, count, k, v, static_cast<cudaStream_t>(stream));
