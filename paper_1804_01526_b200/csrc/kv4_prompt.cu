@@ -398,15 +398,21 @@ kv4_prompt_kernel(const Kv4Attend a) {
 #pragma unroll 1
                 for (int k0 = 0; k0 < 32 / RPL; k0 += UNR) {
                     Eight<T> e[UNR];
+                    if (vec) {
 #pragma unroll
-                    for (int k = 0; k < UNR; ++k) {
-                        const int line = (k0 + k) * RPL + sub;
-                        const int64_t at = __shfl_sync(0xffffffffu, own_at, line);
-                        e[k].zero();
-                        if (128 * t + row0 + line < rows) {
-                            const T* src = reinterpret_cast<const T*>(a.q) + at + 8 * c;
-                            if (vec) e[k].load(src);
-                            else e[k].load_part(src, 8);
+                        for (int k = 0; k < UNR; ++k) {
+                            const int line = (k0 + k) * RPL + sub;
+                            const int64_t at = __shfl_sync(0xffffffffu, own_at, line);
+                            e[k].zero();
+                            if (128 * t + row0 + line < rows) e[k].load(reinterpret_cast<const T*>(a.q) + at + 8 * c);
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < UNR; ++k) {
+                            const int line = (k0 + k) * RPL + sub;
+                            const int64_t at = __shfl_sync(0xffffffffu, own_at, line);
+                            e[k].zero();
+                            if (128 * t + row0 + line < rows) e[k].load_part(reinterpret_cast<const T*>(a.q) + at + 8 * c, 8);
                         }
                     }
 #pragma unroll
