@@ -53,7 +53,7 @@ int launch_kv4_prompt(const Kv4Attend& a, int dtype, cudaStream_t st);
 
 namespace {
 
-constexpr int KA_WARPS = 4, KA_THREADS = 32 * KA_WARPS;
+constexpr int KA_WARPS = 4, KA_THREADS = 32 * KA_WARPS, KA_SPLITS = 8;      // KA_SPLITS: CTAs of a cluster at most
 
 template <int D> struct KaDim {
     static constexpr int NB = D / 32;                      // blocks of a row; words of a key row that a lane takes
@@ -69,7 +69,7 @@ template <int D> struct KaDim {
 template <int D, int NP, int NT> struct KaShared {                      // queries; the rings, then the warps' results in their place; maxima and sums; barriers
     static constexpr int Q = NP * NT * KaDim<D>::STEPS * 256, OP = D + 4;
     static constexpr int RING = KA_WARPS * KaDim<D>::STAGES * KaDim<D>::CHUNK, O = KA_WARPS * 8 * NT * OP * 4;
-    static constexpr int ML = Q + (RING > O ? RING : O), BAR = ML + KA_WARPS * 8 * NT * 8, BYTES = BAR + KA_WARPS * KaDim<D>::STAGES * 8 + 16;
+    static constexpr int ML = Q + (RING > O ? RING : O), BAR = ML + (KA_WARPS + 1) * 8 * NT * 8, BYTES = BAR + KA_WARPS * KaDim<D>::STAGES * 8 + 16;
 };
 
 __device__ __forceinline__ void ka_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint2 b) {
@@ -451,30 +451,61 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
             for (int c = 0; c < 2; ++c) ml[warp * RT + 8 * nt + 2 * t + c] = make_float2(m[nt][c], l[nt][c]);
     }
     __syncthreads();
-    if (splits > 1) cluster_barrier();
+    // the warps' results of one element of four, and in a cluster then the CTAs' (each CTA's lie where its first warp's were)
     const int rank = splits > 1 ? (int)cluster_ctarank() : 0;
-    const uint32_t os_at = smem_u32(os), ml_at = smem_u32(ml);
+    float2* const joined = ml + KA_WARPS * RT;                            // [RT]
+    auto join = [&](int r, int d, float& top, float& sum, float (&v)[4]) {
+        top = -INFINITY;
+        sum = 0.f;
+        v[0] = v[1] = v[2] = v[3] = 0.f;
+#pragma unroll
+        for (int w = 0; w < KA_WARPS; ++w) top = fmaxf(top, ml[w * RT + r].x);
+        if (top == -INFINITY) return;
+#pragma unroll
+        for (int w = 0; w < KA_WARPS; ++w) {
+            const float2 x = ml[w * RT + r];
+            const float f = ka_exp2(x.x - top);
+            const float4 y = *reinterpret_cast<const float4*>(os + (w * RT + r) * OP + d);
+            sum += f * x.y;
+            v[0] += f * y.x; v[1] += f * y.y; v[2] += f * y.z; v[3] += f * y.w;
+        }
+    };
+    if (splits > 1) {
+        for (int i = threadIdx.x; i < rows * (D / 4); i += KA_THREADS) {
+            const int r = i / (D / 4), d = 4 * (i - r * (D / 4));
+            float top, sum, v[4];
+            join(r, d, top, sum, v);
+            *reinterpret_cast<float4*>(os + r * OP + d) = make_float4(v[0], v[1], v[2], v[3]);
+            if (d == 0) joined[r] = make_float2(top, sum);
+        }
+        __syncthreads();
+        cluster_barrier();
+    }
+    const uint32_t os_at = smem_u32(os), joined_at = smem_u32(joined);
     for (int i = rank * KA_THREADS + threadIdx.x; i < rows * (D / 4); i += splits * KA_THREADS) {
         const int r = i / (D / 4), d = 4 * (i - r * (D / 4));
         float top = -INFINITY, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int sp = 0; sp < splits; ++sp) {
-            const uint32_t from = splits > 1 ? map_to_rank(ml_at, sp) : ml_at;
+        if (splits == 1) {
+            join(r, d, top, sum, v);
+        } else {
+            float2 x[KA_SPLITS];
+            float4 y[KA_SPLITS];
 #pragma unroll
-            for (int w = 0; w < KA_WARPS; ++w) top = fmaxf(top, ka_shared2(from + (w * RT + r) * 8).x);
-        }
-        if (top != -INFINITY)
-#pragma unroll 2
-            for (int sp = 0; sp < splits; ++sp) {
-                const uint32_t from = splits > 1 ? map_to_rank(ml_at, sp) : ml_at, of = splits > 1 ? map_to_rank(os_at, sp) : os_at;
-#pragma unroll
-                for (int w = 0; w < KA_WARPS; ++w) {
-                    const float2 x = ka_shared2(from + (w * RT + r) * 8);
-                    const float f = ka_exp2(x.x - top);
-                    const float4 y = ka_shared4(of + ((w * RT + r) * OP + d) * 4);
-                    sum += f * x.y;
-                    v[0] += f * y.x; v[1] += f * y.y; v[2] += f * y.z; v[3] += f * y.w;
+            for (int sp = 0; sp < KA_SPLITS; ++sp)
+                if (sp < splits) {
+                    x[sp] = ka_shared2(map_to_rank(joined_at + r * 8, sp));
+                    y[sp] = ka_shared4(map_to_rank(os_at + (r * OP + d) * 4, sp));
+                    top = fmaxf(top, x[sp].x);
                 }
-            }
+            if (top != -INFINITY)
+#pragma unroll
+                for (int sp = 0; sp < KA_SPLITS; ++sp)
+                    if (sp < splits) {
+                        const float f = ka_exp2(x[sp].x - top);
+                        sum += f * x[sp].y;
+                        v[0] += f * y[sp].x; v[1] += f * y[sp].y; v[2] += f * y[sp].z; v[3] += f * y[sp].w;
+                    }
+        }
         if (slot >= 0) {
             float* part = a.partial + ((int64_t)slot * RT + r) * D + d;
             *reinterpret_cast<float4*>(part) = make_float4(v[0], v[1], v[2], v[3]);
@@ -730,7 +761,7 @@ int ka_launch(Kv4Attend a, cudaStream_t st, size_t* bytes) {
     const dim3 grid((unsigned)a.tiles, (unsigned)a.c.heads, (unsigned)a.c.sequences);
     // Clusters share a tile's keys while that leaves a CTA two units and the GPU has room for twice the CTAs.
     int splits = 1;
-    while (splits < 8 && units > 2 * splits && items * splits * 2 <= ctas) splits *= 2;
+    while (splits < KA_SPLITS && units > 2 * splits && items * splits * 2 <= ctas) splits *= 2;
     // A launch more and the parts' way through memory pay where what is left to a CTA is long and the tiles do not fill the GPU.
     const bool split = units > 12 * splits && items * splits < 2 * (int64_t)ctas && items * units < (1ll << 30);
     if (bytes) {
