@@ -27,11 +27,13 @@ int8_rows_kernel(const T* __restrict__ x, int64_t rows, int64_t k, int64_t ld, b
     if (GROUP <= 32 && row >= rows) return;                          // (whole warps; with larger groups they stay for the barrier)
     const bool in = row < rows;
     const T* src = x + (in ? row : 0) * ld;
-    const int pieces = in ? (int)(pitch / 8) : 0, whole = vec ? (int)(k / 8) : 0;      // of eight values; the row ends inside one of the last two
+    const int pieces = in ? (int)(pitch / 8) : 0, whole = (int)(k / 8);      // of eight values; the row ends inside one of the last two
     Eight<T> v[QR_KEEP];
+    const T* const end = x + (rows - 1) * ld + k;
     auto fetch = [&](int i, Eight<T>& e) {
-        if (i < whole) e.load(src + 8 * (int64_t)i);
-        else e.load_part(src + 8 * (int64_t)i, (int)(k - 8 * (int64_t)i));
+        if (i >= whole) e.load_part(src + 8 * (int64_t)i, (int)(k - 8 * (int64_t)i));
+        else if (vec) e.load(src + 8 * (int64_t)i);
+        else e.load_around(src + 8 * (int64_t)i, x, end);
     };
 #pragma unroll
     for (int u = 0; u < QR_KEEP; ++u) {
@@ -592,7 +594,8 @@ int product(Int8Problem p, const int8_t* a, int64_t lda, const int8_t* b, int64_
 
 }  // namespace
 
-int64_t int8_pitch(int64_t k) { return round_up(k > 0 ? k : 1, 16); }
+// Rows of whole lines of memory for activations that a product converts itself.
+int64_t int8_pitch(int64_t k) { return round_up(k > 0 ? k : 1, k < 128 ? 16 : 128); }
 
 int launch_int8_quantize(const void* x, int dtype, int64_t d0, int64_t d1, int64_t ld, int axis, int8_t* q, int64_t pitch, float* scale, cudaStream_t st) {
     if (dtype == HBFP_F32) return quantize_any(static_cast<const float*>(x), d0, d1, ld, axis, q, pitch, scale, st);

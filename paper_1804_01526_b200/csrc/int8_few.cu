@@ -49,7 +49,7 @@ int8_few_kernel(const FewInt8 p) {
     uint4 a[IF_AHEAD], b[IF_AHEAD];
     auto load = [&](int tile, int c, uint4& u, uint4& v) {
         const int n = tile * IF_CHANNELS + g;
-        const bool there = c < chunks && k0 + 64 * c < p.ldw;
+        const bool there = c < chunks && k0 + 64 * c < p.K;       // (what of the 16 bytes lies behind K meets a zero)
         const int8_t* at = p.w + (int64_t)n * p.ldw + k0 + 64 * c;
         u = v = make_uint4(0u, 0u, 0u, 0u);
         if (there && n < p.N) u = __ldg(reinterpret_cast<const uint4*>(at));

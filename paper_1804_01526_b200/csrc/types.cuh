@@ -98,6 +98,36 @@ struct Eight {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     }
+    // Any alignment, all eight there: whole 16-byte words around them, shifted into place, where those lie within [from, to) (elsewhere as load_part).
+    __device__ __forceinline__ void load_around(const T* p, const void* from, const void* to) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p), first = at & ~(uintptr_t)15;
+        constexpr int Q = sizeof(T) / 2 + 1;                               // 16-byte words of the window
+        if (first < reinterpret_cast<uintptr_t>(from) || first + 16 * Q > reinterpret_cast<uintptr_t>(to)) {
+            load_part(p, 8);
+            return;
+        }
+        uint32_t w[4 * Q];
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(first) + i);
+            w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+        }
+        const uint32_t off = (uint32_t)(at & 15), half = (off & 2) * 8;
+        constexpr int N = 4 * (Q - 1);
+        uint32_t t[4 * Q];
+#pragma unroll
+        for (int i = 0; i < 4 * Q; ++i) t[i] = sizeof(T) == 4 || i + 1 == 4 * Q ? w[i] >> half : __funnelshift_r(w[i], w[i + 1 < 4 * Q ? i + 1 : i], half);
+        uint32_t u[4 * Q];
+#pragma unroll
+        for (int i = 0; i < 4 * Q; ++i) u[i] = (off & 8) && i + 2 < 4 * Q ? t[i + 2 < 4 * Q ? i + 2 : i] : t[i];
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            uint32_t r[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[j] = (off & 4) ? u[4 * i + j + 1] : u[4 * i + j];
+            raw[i] = make_uint4(r[0], r[1], r[2], r[3]);
+        }
+    }
     // The largest magnitude as the bit pattern of an FP32 number (16-bit types: patterns of magnitudes are ordered as their values are, two at a time).
     __device__ __forceinline__ uint32_t amax_bits() const {
         if constexpr (sizeof(T) == 4) {

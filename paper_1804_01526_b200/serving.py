@@ -28,6 +28,14 @@ class Int8Linear(torch.nn.Module):
         self.register_buffer("weight_scale", rows.scale)
         self.register_buffer("bias", None if bias is None else bias.detach().float().contiguous())
 
+    def _apply(self, fn, *args, **kwargs):
+        """Moves like any module; scales and bias stay float32 where the module is given another type (``module.half()``)."""
+        kept = {n: b for n, b in (("weight_scale", self.weight_scale), ("bias", self.bias)) if b is not None}
+        super()._apply(fn, *args, **kwargs)
+        for n, b in kept.items():
+            setattr(self, n, b.to(self.weight_q.device))
+        return self
+
     @classmethod
     def from_hbfp(cls, layer: HbfpLinear) -> "Int8Linear":
         """The layer with the value of a trained ``HbfpLinear``'s weights."""

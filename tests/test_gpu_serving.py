@@ -175,6 +175,58 @@ def test_int8_gemm_views_types_and_what_lies_behind(hb, M):
     assert torch.equal(hb.int8_gemm(x, rows), hb.int8_gemm(x, w)[:, 5:40])
 
 
+@pytest.mark.parametrize("M,N,K", [(1, 40, 30000), (3, 100, 13000), (3, 24, 14400), (2, 5000, 96), (4, 33, 30000)])
+def test_int8_gemm_few_tokens_long_contractions(hb, M, N, K):
+    """Tokens that fit the one-launch kernel's shared memory and ones that do not."""
+    g = gen(K)
+    x, w = normal(g, M, K).bfloat16(), hb.int8_quantize(normal(g, N, K))
+    check_product(hb, x, w, None, hb.int8_gemm(x, w))
+
+
+@pytest.mark.parametrize("M", [2, 9, 200])
+def test_int8_gemm_of_part_of_a_larger_matrix(hb, M):
+    """Channels and contraction are a window of wider weights, up to its last byte."""
+    g = gen(M + 50)
+    big = hb.int8_quantize(normal(g, 64, 512))
+    w = hb.Int8Rows(big.q[16:, 256:], big.scale[16:], 250)
+    x = normal(g, M, 250)
+    check_product(hb, x, w, None, hb.int8_gemm(x, w))
+
+
+def test_int8_runs_in_a_graph_and_on_another_stream(hb):
+    g = gen(77)
+    for M, N, K in ((1, 256, 512), (20, 300, 500), (2048, 1536, 256)):
+        x, w = normal(g, M, K).half(), hb.int8_quantize(normal(g, N, K))
+        want = hb.int8_gemm(x, w)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            y = hb.int8_gemm(x, w)
+        side.synchronize()
+        assert torch.equal(y, want)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            y = hb.int8_gemm(x, w)
+        x.copy_(normal(g, M, K))
+        graph.replay()
+        assert torch.equal(y, hb.int8_gemm(x, w))
+
+
+def test_int8_linear_keeps_its_scales(hb):
+    """A module given another type keeps FP32 scales; its product is the function's."""
+    from paper_1804_01526_b200.serving import Int8Linear
+    g = gen(5)
+    layer = Int8Linear(normal(g, 96, 40), normal(g, 40)).half()
+    assert layer.weight_scale.dtype == layer.bias.dtype == torch.float32 and layer.weight_q.dtype == torch.int8
+    x = normal(g, 2, 3, 96).half()
+    y = layer(x)
+    assert y.shape == (2, 3, 40) and y.dtype == torch.float16 and not y.requires_grad
+    check_product(hb, x.view(6, 96), hb.Int8Rows(layer.weight_q, layer.weight_scale, 96), layer.bias, y.view(6, 40))
+    again = Int8Linear(torch.zeros(96, 40, device="cuda"), torch.zeros(40, device="cuda"))
+    again.load_state_dict(layer.state_dict())
+    assert torch.equal(again(x), y)
+
+
 def test_int8_gemm_of_nothing(hb):
     w = hb.int8_quantize(normal(gen(0), 8, 32))
     assert hb.int8_gemm(torch.empty(0, 32, device="cuda"), w).shape == (0, 8)
