@@ -167,6 +167,40 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
     uint2* qs = reinterpret_cast<uint2*>(sm);                             // [NP][NT][STEPS][32]
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // (copies follow where results were written)
     __syncthreads();                                                      // the tile before is through with shared memory
+    // ---- the ring. Lanes 0 to 3 each ask for one of a chunk's arrays (keys, values, their exponents); every lane knows the page of the
+    // chunk after the last one asked for. gone: which sixteens of each stage's chunk are not there, two bits a stage.
+    const uint32_t base = smem_u32(sm) + KaShared<D, NP, NT>::Q + warp * C::STAGES * C::CHUNK;
+    constexpr int GROUPS = C::CH / 16;
+    const int mine = lane & 3;
+    const uint32_t line = mine < 2 ? D / 2 : C::NB, to_mine = (mine & 1) * (mine < 2 ? C::MANT : C::EXPS) + (mine < 2 ? 0 : 2 * C::MANT);
+    const int64_t page_bytes = ((int64_t)a.c.heads << a.c.shift) * line;
+    const char* const array = reinterpret_cast<const char*>(mine == 0 ? (const void*)a.c.k_mant : mine == 1 ? (const void*)a.c.v_mant : mine == 2 ? (const void*)a.c.k_exps
+                                                                                                                                       : (const void*)a.c.v_exps) +
+                              ((int64_t)h << a.c.shift) * line;
+    const bool small = GROUPS == 2 && a.c.shift == 4;                      // pages of sixteen rows: the second half of a chunk has its own
+    auto page_of = [&](int p) { return p < range.hi ? (int)kv4_page(a.c, b, p >> a.c.shift) : -1; };
+    auto ask = [&](int p, int id, int stage) {
+        const uint32_t at = base + stage * C::CHUNK + to_mine, bar = ring.bars + 8 * stage;
+        const uint32_t keys = id < 0 ? 0u : small ? 16u : (uint32_t)C::CH;
+        const int id2 = small ? page_of(p + 16) : -1;
+        if (lane == 0) mbar_expect_tx(bar, (keys + (id2 >= 0 ? 16u : 0u)) * (2 * (D / 2 + C::NB)));
+        __syncwarp();
+        if (lane < 4) {
+            const char* src = array + (uint32_t)(p & (a.c.page - 1)) * line;
+            if (id >= 0) ka_copy(at, src + id * page_bytes, keys * line, bar);
+            if (small && id2 >= 0) ka_copy(at + 16 * line, array + id2 * page_bytes, 16 * line, bar);
+        }
+        return (id < 0 ? (small ? 1 : 3) : 0) | (small && id2 < 0 ? 2 : 0);
+    };
+    const int start = range.lo + warp * C::CH;
+    int gone = 0;
+#pragma unroll
+    for (int i = 0; i < C::STAGES - 1; ++i) {
+        const int p = start + i * C::UNIT;
+        if (p < range.hi) gone |= ask(p, page_of(p), i) << (2 * i);
+    }
+    int next_id = page_of(start + (C::STAGES - 1) * C::UNIT);
+    // ---- the queries, while the first keys come
     for (int i = threadIdx.x; i < NT * C::STEPS * 32; i += KA_THREADS) {
         const int l = i & 31, step = (i >> 5) % C::STEPS, nt = (i >> 5) / C::STEPS, r = 8 * nt + (l >> 2);
         float e[4] = {0.f, 0.f, 0.f, 0.f};
@@ -204,39 +238,6 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
 #pragma unroll
         for (int c = 0; c < 2; ++c) { m[nt][c] = -INFINITY; l[nt][c] = 0.f; }
 
-    // ---- the ring. Lanes 0 to 3 each ask for one of a chunk's arrays (keys, values, their exponents); every lane knows the page of the
-    // chunk after the last one asked for. gone: which sixteens of each stage's chunk are not there, two bits a stage.
-    const uint32_t base = smem_u32(sm) + KaShared<D, NP, NT>::Q + warp * C::STAGES * C::CHUNK;
-    constexpr int GROUPS = C::CH / 16;
-    const int mine = lane & 3;
-    const uint32_t line = mine < 2 ? D / 2 : C::NB, to_mine = (mine & 1) * (mine < 2 ? C::MANT : C::EXPS) + (mine < 2 ? 0 : 2 * C::MANT);
-    const int64_t page_bytes = ((int64_t)a.c.heads << a.c.shift) * line;
-    const char* const array = reinterpret_cast<const char*>(mine == 0 ? (const void*)a.c.k_mant : mine == 1 ? (const void*)a.c.v_mant : mine == 2 ? (const void*)a.c.k_exps
-                                                                                                                                       : (const void*)a.c.v_exps) +
-                              ((int64_t)h << a.c.shift) * line;
-    const bool small = GROUPS == 2 && a.c.shift == 4;                      // pages of sixteen rows: the second half of a chunk has its own
-    auto page_of = [&](int p) { return p < range.hi ? (int)kv4_page(a.c, b, p >> a.c.shift) : -1; };
-    auto ask = [&](int p, int id, int stage) {
-        const uint32_t at = base + stage * C::CHUNK + to_mine, bar = ring.bars + 8 * stage;
-        const uint32_t keys = id < 0 ? 0u : small ? 16u : (uint32_t)C::CH;
-        const int id2 = small ? page_of(p + 16) : -1;
-        if (lane == 0) mbar_expect_tx(bar, (keys + (id2 >= 0 ? 16u : 0u)) * (2 * (D / 2 + C::NB)));
-        __syncwarp();
-        if (lane < 4) {
-            const char* src = array + (uint32_t)(p & (a.c.page - 1)) * line;
-            if (id >= 0) ka_copy(at, src + id * page_bytes, keys * line, bar);
-            if (small && id2 >= 0) ka_copy(at + 16 * line, array + id2 * page_bytes, 16 * line, bar);
-        }
-        return (id < 0 ? (small ? 1 : 3) : 0) | (small && id2 < 0 ? 2 : 0);
-    };
-    const int start = range.lo + warp * C::CH;
-    int gone = 0;
-#pragma unroll
-    for (int i = 0; i < C::STAGES - 1; ++i) {
-        const int p = start + i * C::UNIT;
-        if (p < range.hi) gone |= ask(p, page_of(p), i) << (2 * i);
-    }
-    int next_id = page_of(start + (C::STAGES - 1) * C::UNIT);
     // row of this lane's keys g and g + 8 in the chunk: neighbours are swapped in every other pair, so that neither the keys' nor the values'
     // accesses meet in a bank more than twice
     const int gk = g ^ ((g >> 1) & 1), ke0 = (t * C::NB) >> 2, ve0 = (g * C::VW) >> 2;
@@ -570,14 +571,14 @@ __device__ __forceinline__ int2 ka_units(const Kv4Attend& a, const Kv4Seq& s) {
     const int tiles = (s.n * a.group + 8 * NT - 1) / (8 * NT) * a.c.heads;
     return make_int2(max(1, (r.hi - r.lo + KaDim<D>::UNIT - 1) / KaDim<D>::UNIT), tiles);
 }
-// Units of all sequences and of those before each thread's share of them, by all threads of the CTA.
+// Units of all sequences, of those before each thread's share of them and of its own, by all threads of the CTA.
 template <int D, int NT, int WARPS>
-__device__ __forceinline__ void ka_scan(const Kv4Attend& a, int& total, int& before, int& b0, int& b1) {
+__device__ __forceinline__ void ka_scan(const Kv4Attend& a, int& total, int& before, int& own, int& b0, int& b1) {
     __shared__ int sums[WARPS];
     const int per = (a.c.sequences + 32 * WARPS - 1) / (32 * WARPS);
     b0 = min(a.c.sequences, (int)threadIdx.x * per);
     b1 = min(a.c.sequences, b0 + per);
-    int own = 0;
+    own = 0;
     for (int b = b0; b < b1; ++b) {
         const int2 u = ka_units<D, NT>(a, kv4_seq(a.c, b));
         own += u.x * u.y;
@@ -606,16 +607,21 @@ kv4_attend_split_kernel(const Kv4Attend a) {
     __shared__ int found[2];
     KaRing ring = ka_ring<D, NP, NT>(sm);
     chain_start();
-    int total, before, b0, b1;
-    ka_scan<D, NT, KA_WARPS>(a, total, before, b0, b1);
+    int total, before, own, b0, b1;
+    ka_scan<D, NT, KA_WARPS>(a, total, before, own, b0, b1);
     const int ctas = min(a.ctas, total), cta = blockIdx.x;
     if (cta >= ctas) return;
     int u = (int)((int64_t)total * cta / ctas);
     const int end = (int)((int64_t)total * (cta + 1) / ctas);
-    for (int b = b0; b < b1; ++b) {
-        const int2 x = ka_units<D, NT>(a, kv4_seq(a.c, b));
-        if (u >= before && u < before + x.x * x.y) { found[0] = b; found[1] = u - before; }
-        before += x.x * x.y;
+    if (u >= before && u < before + own) {
+        int b = b0;
+        for (; b + 1 < b1; ++b) {
+            const int2 x = ka_units<D, NT>(a, kv4_seq(a.c, b));
+            if (u < before + x.x * x.y) break;
+            before += x.x * x.y;
+        }
+        found[0] = b;
+        found[1] = u - before;
     }
     __syncthreads();
     int b = found[0], at = found[1];
@@ -651,8 +657,8 @@ kv4_join_kernel(const Kv4Attend a, int each) {
     __shared__ float weights[GROUPS];
     chain_start();
     const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x / (RT / each), row0 = blockIdx.x % (RT / each) * each;
-    int total, before, b0, b1;
-    ka_scan<D, NT, KJ_THREADS / 32>(a, total, before, b0, b1);
+    int total, before, own, b0, b1;
+    ka_scan<D, NT, KJ_THREADS / 32>(a, total, before, own, b0, b1);
     const Kv4Seq s = kv4_seq(a.c, b);
     const int2 x = ka_units<D, NT>(a, s);
     const int item = tile * a.c.heads + h;
