@@ -42,7 +42,7 @@ kv4_append_kernel(const Kv4Args a, const T* __restrict__ k, Kv4Rows ks, const T*
     using W = Kv4Words<D>;
     chain_start();
     const int b = blockIdx.y;
-    const Kv4Seq s = kv4_seq(a, b);
+    const Kv4Seq s = kv4_seq_unreported(a, b);
     const W w(a.heads);
     // every lane of a warp stays for the shuffles
     for (int64_t t0 = (int64_t)blockIdx.x * w.tokens; t0 < s.n; t0 += (int64_t)gridDim.x * w.tokens * KV4_UNROLL)
@@ -84,6 +84,7 @@ kv4_append_kernel(const Kv4Args a, const T* __restrict__ k, Kv4Rows ks, const T*
                 if ((word & 3) == 0) (side ? a.v_exps : a.k_exps)[row[u] * W::NB + (word >> 2)] = (int8_t)exp;
             }
         }
+    kv4_report(a, s);
 }
 
 // The values of the last `count` positions of every sequence, FP32 [sequences * count][heads][dim]; zeros where there is no position.
@@ -95,7 +96,7 @@ kv4_read_kernel(Kv4Args a, int count, float* __restrict__ k, float* __restrict__
     const int b = blockIdx.y;
     a.starts = nullptr;
     a.most = count;
-    const Kv4Seq s = kv4_seq(a, b);
+    const Kv4Seq s = kv4_seq_unreported(a, b);
     const W w(a.heads);
     if (w.idle()) return;
     for (int64_t t0 = (int64_t)blockIdx.x * w.tokens; t0 < s.n; t0 += (int64_t)gridDim.x * w.tokens * KV4_UNROLL)
@@ -128,6 +129,7 @@ kv4_read_kernel(Kv4Args a, int count, float* __restrict__ k, float* __restrict__
                              "f"(e[6]), "f"(e[7]) : "memory");
             }
         }
+    kv4_report(a, s);
 }
 
 // CTAs of a sequence: one for what it takes at a time, several times as much for a CTA where that leaves the GPU its fill.

@@ -40,10 +40,12 @@ namespace {
 struct Kv4Seq {
     int64_t first;      // its first row among the call's tokens
     int n, length;      // tokens of this call, tokens in the cache when they are in it
+    bool bad;           // one of the numbers was out of range
 };
 
-// The numbers come from the caller's device memory: whatever they are, a row lies within the call's tokens and a position within the table.
-__device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Args& a, int b) {
+// The numbers come from the caller's device memory: whatever they are, a row lies within the call's tokens and a position within the table. (Not
+// reported here: a branch on the length would keep loads that do not need it waiting.)
+__device__ __forceinline__ Kv4Seq kv4_seq_unreported(const Kv4Args& a, int b) {
     Kv4Seq s;
     bool bad = false;
     if (a.starts) {
@@ -60,7 +62,15 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Args& a, int b) {
     const int len = __ldg(a.lengths + b);
     s.length = len < 0 ? 0 : len;
     if (s.length > cap) { bad = true; s.length = (int)cap; }
-    if (bad) atomicCAS(a.status, 0, STATUS_TOKENS);
+    s.bad = bad;
+    return s;
+}
+__device__ __forceinline__ void kv4_report(const Kv4Args& a, const Kv4Seq& s) {
+    if (s.bad) atomicCAS(a.status, 0, STATUS_TOKENS);
+}
+__device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Args& a, int b) {
+    const Kv4Seq s = kv4_seq_unreported(a, b);
+    kv4_report(a, s);
     return s;
 }
 

@@ -12,13 +12,14 @@
 // has bits (1 for bfloat16, 2 for binary16, 3 for FP32: of a query nothing is left, of a probability 2^-8, 2^-16, 2^-24), so
 // products are exact and sums FP32. Softmax in base 2, running maximum and sum in FP32.
 //
-// Bound: reading the cache, dim / 2 + dim / 32 bytes per key and head and as much for values. Warps take 32 keys each in turn (16 of a
-// 256-wide head) and keep their own maximum and sum; the CTA joins them once at the end of its keys. Keys, values and exponents of a warp's
+// Bound: reading the cache, dim / 2 + dim / 32 bytes per key and head and as much for values. Warps take 64 keys each in turn (32 where
+// a tile has more than eight rows, 16 of a 256-wide head) and keep their own maximum and sum; the CTA joins them once at the end of its keys. Keys, values and exponents of a warp's
 // next chunks come by bulk copies into its own ring of shared memory (rows of a page and head are one run of memory), issued by one
-// lane, so that a warp has two chunks in flight without a register or an address for them.
+// lane, so that a warp has its next chunks in flight without a register or an address for them (64 keys at a time with 12 warps an SM 94.6 us for
+// 64 sequences of up to 8192 tokens, 32 with 16 warps 97.4; one sequence of 131072 in binary16 52.4 / 57.8).
 //
 // Split. Sequences differ in length and the host does not know the lengths, so a launch with long keys has as many CTAs as the GPU
-// holds at a time and each takes an equal share of all units (128 keys of one sequence, head and row tile), found by adding up the
+// holds at a time and each takes an equal share of all units (a chunk for each warp, of one sequence, head and row tile), found by adding up the
 // lengths itself. A tile whose keys end up in several CTAs leaves FP32 parts (at most two a CTA) that a second launch joins in
 // ascending order: the same result every time.
 #pragma once
@@ -55,21 +56,21 @@ namespace {
 
 constexpr int KA_WARPS = 4, KA_THREADS = 32 * KA_WARPS, KA_SPLITS = 8;      // KA_SPLITS: CTAs of a cluster at most
 
-template <int D> struct KaDim {
+template <int D, int NT> struct KaDim {
     static constexpr int NB = D / 32;                      // blocks of a row; words of a key row that a lane takes
     static constexpr int VW = (D + 63) / 64;               // words of a value row that a lane takes (96: as 128, the last lanes none)
-    static constexpr int CH = D <= 128 ? 32 : 16;          // keys of a warp at a time
+    static constexpr int CH = D > 128 ? 16 : NT == 1 ? 64 : 32;      // keys of a warp at a time
     static constexpr int UNIT = CH * KA_WARPS;             // keys of a CTA at a time
     static constexpr int STEPS = D / 16;                   // MMA steps along a key row
     static constexpr int KE = D == 128 || D == 64 ? 1 : 2; // exponents of a lane's key words
     // a chunk in shared memory: keys, values, exponents of the keys, of the values
-    static constexpr int MANT = CH * D / 2, EXPS = CH * NB, CHUNK = 2 * (MANT + EXPS), STAGES = 3;
+    static constexpr int MANT = CH * D / 2, EXPS = CH * NB, CHUNK = 2 * (MANT + EXPS), STAGES = CH == 64 ? 2 : 3;
     static_assert(MANT % 16 == 0 && EXPS % 16 == 0, "bulk copies");
 };
 template <int D, int NP, int NT> struct KaShared {                      // queries; the rings, then the warps' results in their place; maxima and sums; barriers
-    static constexpr int Q = NP * NT * KaDim<D>::STEPS * 256, OP = D + 4;
-    static constexpr int RING = KA_WARPS * KaDim<D>::STAGES * KaDim<D>::CHUNK, O = KA_WARPS * 8 * NT * OP * 4;
-    static constexpr int ML = Q + (RING > O ? RING : O), BAR = ML + (KA_WARPS + 1) * 8 * NT * 8, BYTES = BAR + KA_WARPS * KaDim<D>::STAGES * 8 + 16;
+    static constexpr int Q = NP * NT * KaDim<D, NT>::STEPS * 256, OP = D + 4;
+    static constexpr int RING = KA_WARPS * KaDim<D, NT>::STAGES * KaDim<D, NT>::CHUNK, O = KA_WARPS * 8 * NT * OP * 4;
+    static constexpr int ML = Q + (RING > O ? RING : O), BAR = ML + (KA_WARPS + 1) * 8 * NT * 8, BYTES = BAR + KA_WARPS * KaDim<D, NT>::STAGES * 8 + 16;
 };
 
 __device__ __forceinline__ void ka_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint2 b) {
@@ -159,7 +160,7 @@ struct KaRange { int lo, hi; };
 // tile's keys each and join them here.
 template <int D, int NP, int NT, class T>
 __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq& seq, int h, int tile, KaRange range, int slot, int splits, unsigned char* sm, KaRing& ring) {
-    using C = KaDim<D>;
+    using C = KaDim<D, NT>;
     constexpr int RT = 8 * NT, MT = C::CH / 16, TILES = 4 * C::VW;        // TILES: 16-row tiles of V^T
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int rows = min(RT, seq.n * a.group - tile * RT), r0 = tile * RT;
@@ -168,36 +169,43 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // (copies follow where results were written)
     __syncthreads();                                                      // the tile before is through with shared memory
     // ---- the ring. Lanes 0 to 3 each ask for one of a chunk's arrays (keys, values, their exponents); every lane knows the page of the
-    // chunk after the last one asked for. gone: which sixteens of each stage's chunk are not there, two bits a stage.
+    // chunk after the last one asked for. gone: which sixteens of each stage's chunk are not there.
     const uint32_t base = smem_u32(sm) + KaShared<D, NP, NT>::Q + warp * C::STAGES * C::CHUNK;
-    constexpr int GROUPS = C::CH / 16;
+    constexpr int GROUPS = C::CH / 16, ALL = (1 << GROUPS) - 1;
     const int mine = lane & 3;
     const uint32_t line = mine < 2 ? D / 2 : C::NB, to_mine = (mine & 1) * (mine < 2 ? C::MANT : C::EXPS) + (mine < 2 ? 0 : 2 * C::MANT);
     const int64_t page_bytes = ((int64_t)a.c.heads << a.c.shift) * line;
     const char* const array = reinterpret_cast<const char*>(mine == 0 ? (const void*)a.c.k_mant : mine == 1 ? (const void*)a.c.v_mant : mine == 2 ? (const void*)a.c.k_exps
                                                                                                                                        : (const void*)a.c.v_exps) +
                               ((int64_t)h << a.c.shift) * line;
-    const bool small = GROUPS == 2 && a.c.shift == 4;                      // pages of sixteen rows: the second half of a chunk has its own
+    // a chunk in pages of fewer rows: a page for each of its pieces
+    const int piece = min(C::CH, a.c.page), pieces = C::CH / piece, groups = piece / 16;
     auto page_of = [&](int p) { return p < range.hi ? (int)kv4_page(a.c, b, p >> a.c.shift) : -1; };
     auto ask = [&](int p, int id, int stage) {
         const uint32_t at = base + stage * C::CHUNK + to_mine, bar = ring.bars + 8 * stage;
-        const uint32_t keys = id < 0 ? 0u : small ? 16u : (uint32_t)C::CH;
-        const int id2 = small ? page_of(p + 16) : -1;
-        if (lane == 0) mbar_expect_tx(bar, (keys + (id2 >= 0 ? 16u : 0u)) * (2 * (D / 2 + C::NB)));
+        int ids[GROUPS], keys = 0, gone = 0;
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i)
+            if (i < pieces) {
+                ids[i] = i == 0 ? id : page_of(p + i * piece);
+                if (ids[i] >= 0) keys += piece;
+                else gone |= ((1 << groups) - 1) << (i * groups);
+            }
+        if (lane == 0) mbar_expect_tx(bar, (uint32_t)keys * (2 * (D / 2 + C::NB)));
         __syncwarp();
-        if (lane < 4) {
-            const char* src = array + (uint32_t)(p & (a.c.page - 1)) * line;
-            if (id >= 0) ka_copy(at, src + id * page_bytes, keys * line, bar);
-            if (small && id2 >= 0) ka_copy(at + 16 * line, array + id2 * page_bytes, 16 * line, bar);
-        }
-        return (id < 0 ? (small ? 1 : 3) : 0) | (small && id2 < 0 ? 2 : 0);
+        if (lane < 4)
+#pragma unroll
+            for (int i = 0; i < GROUPS; ++i)
+                if (i < pieces && ids[i] >= 0)
+                    ka_copy(at + i * piece * line, array + ids[i] * page_bytes + (uint32_t)((p + i * piece) & (a.c.page - 1)) * line, piece * line, bar);
+        return gone;
     };
     const int start = range.lo + warp * C::CH;
     int gone = 0;
 #pragma unroll
     for (int i = 0; i < C::STAGES - 1; ++i) {
         const int p = start + i * C::UNIT;
-        if (p < range.hi) gone |= ask(p, page_of(p), i) << (2 * i);
+        if (p < range.hi) gone |= ask(p, page_of(p), i) << (GROUPS * i);
     }
     int next_id = page_of(start + (C::STAGES - 1) * C::UNIT);
     // ---- the queries, while the first keys come
@@ -249,11 +257,11 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
         {
             const int p = pos + (C::STAGES - 1) * C::UNIT, to = stage == 0 ? C::STAGES - 1 : stage - 1;
             if (p < range.hi) {
-                gone = (gone & ~(3 << (2 * to))) | ask(p, next_id, to) << (2 * to);
+                gone = (gone & ~(ALL << (GROUPS * to))) | ask(p, next_id, to) << (GROUPS * to);
                 next_id = page_of(p + C::UNIT);
             }
         }
-        const int missing = gone >> (2 * stage) & 3;
+        const int missing = gone >> (GROUPS * stage) & ALL;
         ok = mbar_wait_warp_soon(ring.bars + 8 * stage, ring.phases >> stage & 1, ring.abort_flag, a.c.status, 187);
         if (!ok) break;
         ring.phases ^= 1u << stage;
@@ -524,7 +532,7 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
 template <int D, int NP, int NT>
 __device__ __forceinline__ KaRing ka_ring(unsigned char* sm) {
     using S = KaShared<D, NP, NT>;
-    constexpr int STAGES = KaDim<D>::STAGES;
+    constexpr int STAGES = KaDim<D, NT>::STAGES;
     volatile int* flag = reinterpret_cast<volatile int*>(sm + S::BAR + KA_WARPS * STAGES * 8);
     const uint32_t bars = smem_u32(sm + S::BAR);
     if (threadIdx.x == 0) {
@@ -541,20 +549,20 @@ __device__ __forceinline__ KaRange ka_range(const Kv4Attend& a, const Kv4Seq& s,
     KaRange r;
     const int base = s.length - s.n;
     r.hi = max(0, min(s.length, base + last_query + 1));
-    r.lo = a.window ? max(0, base + first_query - a.window + 1) & ~31 : 0;
+    r.lo = a.window ? max(0, base + first_query - a.window + 1) & ~63 : 0;
     return r;
 }
 
 // A tile per CTA, or per cluster of `splits` CTAs: short keys, or tiles enough.
 template <int D, int NP, int NT, class T>
-__global__ void __launch_bounds__(KA_THREADS, NT == 1 && D <= 128 ? 4 : 2)
+__global__ void __launch_bounds__(KA_THREADS, NT == 1 && D <= 128 ? 3 : 2)
 kv4_attend_kernel(const Kv4Attend a, int splits) {
     extern __shared__ __align__(128) unsigned char sm[];
     KaRing ring = ka_ring<D, NP, NT>(sm);
     chain_start();
     const int b = blockIdx.z, h = blockIdx.y, tile = blockIdx.x / splits, rank = blockIdx.x % splits;
     const Kv4Seq s = kv4_seq(a.c, b);
-    constexpr int RT = 8 * NT, UNIT = KaDim<D>::UNIT;
+    constexpr int RT = 8 * NT, UNIT = KaDim<D, NT>::UNIT;
     if (tile * RT >= s.n * a.group) return;                               // (all of a cluster alike)
     const int last = min((tile + 1) * RT, s.n * a.group) - 1;
     KaRange r = ka_range(a, s, tile * RT / a.group, last / a.group);
@@ -569,7 +577,7 @@ template <int D, int NT>
 __device__ __forceinline__ int2 ka_units(const Kv4Attend& a, const Kv4Seq& s) {
     const KaRange r = ka_range(a, s, 0, s.n - 1);
     const int tiles = (s.n * a.group + 8 * NT - 1) / (8 * NT) * a.c.heads;
-    return make_int2(max(1, (r.hi - r.lo + KaDim<D>::UNIT - 1) / KaDim<D>::UNIT), tiles);
+    return make_int2(max(1, (r.hi - r.lo + KaDim<D, NT>::UNIT - 1) / KaDim<D, NT>::UNIT), tiles);
 }
 // Units of all sequences, of those before each thread's share of them and of its own, by all threads of the CTA.
 template <int D, int NT, int WARPS>
@@ -601,7 +609,7 @@ __device__ __forceinline__ void ka_scan(const Kv4Attend& a, int& total, int& bef
 }
 
 template <int D, int NP, int NT, class T>
-__global__ void __launch_bounds__(KA_THREADS, NT == 1 && D <= 128 ? 4 : 2)
+__global__ void __launch_bounds__(KA_THREADS, NT == 1 && D <= 128 ? 3 : 2)
 kv4_attend_split_kernel(const Kv4Attend a) {
     extern __shared__ __align__(128) unsigned char sm[];
     __shared__ int found[2];
@@ -633,8 +641,8 @@ kv4_attend_split_kernel(const Kv4Attend a) {
             const int item = at / x.x, within = at - item * x.x, take = min(x.x - within, end - u);
             const int tile = item / a.c.heads, h = item - tile * a.c.heads;
             KaRange r;
-            r.lo = all.lo + within * KaDim<D>::UNIT;
-            r.hi = min(all.hi, r.lo + take * KaDim<D>::UNIT);
+            r.lo = all.lo + within * KaDim<D, NT>::UNIT;
+            r.hi = min(all.hi, r.lo + take * KaDim<D, NT>::UNIT);
             const int slot = take == x.x ? -1 : 2 * cta + (within == 0);
             ka_tile<D, NP, NT, T>(a, b, s, h, tile, r, slot, 1, sm, ring);
             at += take;
@@ -763,13 +771,13 @@ int ka_launch(Kv4Attend a, cudaStream_t st, size_t* bytes) {
     const int64_t cap = (int64_t)a.c.table_pages << a.c.shift;
     const int64_t keys = a.window && (int64_t)a.window + a.c.most + 15 < cap ? (int64_t)a.window + a.c.most + 15 : cap;
     a.tiles = (int)(((int64_t)a.c.most * a.group + RT - 1) / RT);
-    const int64_t items = (int64_t)a.tiles * a.c.heads * a.c.sequences, units = (keys + KaDim<D>::UNIT - 1) / KaDim<D>::UNIT;
+    const int64_t items = (int64_t)a.tiles * a.c.heads * a.c.sequences, units = (keys + KaDim<D, NT>::UNIT - 1) / KaDim<D, NT>::UNIT;
     const dim3 grid((unsigned)a.tiles, (unsigned)a.c.heads, (unsigned)a.c.sequences);
     // Clusters share a tile's keys while that leaves a CTA two units and the GPU has room for twice the CTAs.
     int splits = 1;
-    while (splits < KA_SPLITS && units > 2 * splits && items * splits * 2 <= ctas) splits *= 2;
+    while (splits < KA_SPLITS && keys > 256 * splits && items * splits * 2 <= ctas) splits *= 2;
     // A launch more and the parts' way through memory pay where what is left to a CTA is long and the tiles do not fill the GPU.
-    const bool split = units > 12 * splits && items * splits < 2 * (int64_t)ctas && items * units < (1ll << 30);
+    const bool split = keys > 1536 * splits && items * splits < 2 * (int64_t)ctas && items * units < (1ll << 30);
     if (bytes) {
         *bytes = split ? (size_t)2 * ctas * RT * (D + 2) * sizeof(float) : 0;
         return HBFP_OK;
