@@ -67,7 +67,7 @@ int attend(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int dtype, 
         a->c.status = device_status_word();
         if (!a->c.status) return HBFP_ERR_CUDA;
     }
-    if (kv4_prompt_eligible(*a)) return bytes ? (int)HBFP_OK : launch_kv4_prompt(*a, dtype, st);
+    if (kv4_prompt_eligible(*a, dtype)) return bytes ? (int)HBFP_OK : launch_kv4_prompt(*a, dtype, st);
     if (dtype == HBFP_F32) return launch_kv4_attend_f32(*a, st, bytes);
     if (dtype == HBFP_BF16) return launch_kv4_attend_bf16(*a, st, bytes);
     return launch_kv4_attend_f16(*a, st, bytes);
@@ -84,7 +84,7 @@ int hbfp_int8_quantize(const void* x, int dtype, int64_t d0, int64_t d1, int64_t
     if (!dtype_ok(dtype) || d0 < 0 || d1 < 0 || ld < d1 || (contract_axis != 0 && contract_axis != 1)) return HBFP_ERR_INVALID_ARG;
     const int64_t rows = contract_axis == 1 ? d0 : d1, k = contract_axis == 1 ? d1 : d0;
     if (pitch < k || pitch < 16) return HBFP_ERR_INVALID_ARG;
-    if (rows >= MOST || k >= MOST) return HBFP_ERR_UNSUPPORTED;
+    if (rows >= MOST || k >= MOST || pitch >= 2 * MOST) return HBFP_ERR_UNSUPPORTED;
     if (rows > 0 && (!q || !scale || (k > 0 && !x))) return HBFP_ERR_INVALID_ARG;
     if (pitch % 16 != 0 || !aligned(q, 16)) return HBFP_ERR_ALIGNMENT;
     return launch_int8_quantize(x, dtype, d0, d1, ld, contract_axis, q, pitch, scale, static_cast<cudaStream_t>(stream));
@@ -142,7 +142,7 @@ int hbfp_kv4_append(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, in
 }
 
 int hbfp_kv4_read(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int32_t count, float* k, float* v, void* stream) {
-    if (!batch || count < 0) return HBFP_ERR_INVALID_ARG;
+    if (!batch || batch->struct_size != sizeof(*batch) || count < 0) return HBFP_ERR_INVALID_ARG;
     hbfp_kv4_batch all = *batch;
     all.starts = nullptr;
     all.max_tokens = count;

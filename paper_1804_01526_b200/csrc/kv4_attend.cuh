@@ -45,11 +45,17 @@ struct Kv4Attend {
     int ctas;
 };
 
+// Keys that a sequence's rows see at most, of what the host knows (whole chunks of 64 from the window's edge on).
+inline int64_t kv4_keys(const Kv4Attend& a) {
+    const int64_t cap = (int64_t)a.c.table_pages << a.c.shift, near = (int64_t)a.window + a.c.most + 63;
+    return a.window && near < cap ? near : cap;
+}
+
 int launch_kv4_attend_f32(const Kv4Attend& a, cudaStream_t st, size_t* bytes);
 int launch_kv4_attend_bf16(const Kv4Attend& a, cudaStream_t st, size_t* bytes);
 int launch_kv4_attend_f16(const Kv4Attend& a, cudaStream_t st, size_t* bytes);
 // Many rows of a 64- or 128-wide head (kv4_prompt.cu); no workspace.
-bool kv4_prompt_eligible(const Kv4Attend& a);
+bool kv4_prompt_eligible(const Kv4Attend& a, int dtype);
 int launch_kv4_prompt(const Kv4Attend& a, int dtype, cudaStream_t st);
 
 namespace {
@@ -231,7 +237,7 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
 #pragma unroll
         for (int c = 0; c < 2; ++c) limit[nt][c] = seq.length - seq.n + (r0 + min(8 * nt + 2 * t + c, rows - 1)) / a.group;
     const int first_limit = seq.length - seq.n + r0 / a.group, last_limit = seq.length - seq.n + (r0 + rows - 1) / a.group;
-    const int window = a.window ? a.window : 0x7fffffff;
+    const int window = a.window ? a.window : 1 << 30;
     __syncthreads();
 
     float o[TILES][NT][4], m[NT][2], l[NT][2];
@@ -469,11 +475,11 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
         v[0] = v[1] = v[2] = v[3] = 0.f;
 #pragma unroll
         for (int w = 0; w < KA_WARPS; ++w) top = fmaxf(top, ml[w * RT + r].x);
-        if (top == -INFINITY) return;
+        const float use = top == -INFINITY ? 0.f : top;                   // (no key seen, or scores that are no numbers: these stay so)
 #pragma unroll
         for (int w = 0; w < KA_WARPS; ++w) {
             const float2 x = ml[w * RT + r];
-            const float f = ka_exp2(x.x - top);
+            const float f = ka_exp2(x.x - use);
             const float4 y = *reinterpret_cast<const float4*>(os + (w * RT + r) * OP + d);
             sum += f * x.y;
             v[0] += f * y.x; v[1] += f * y.y; v[2] += f * y.z; v[3] += f * y.w;
@@ -506,14 +512,14 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
                     y[sp] = ka_shared4(map_to_rank(os_at + (r * OP + d) * 4, sp));
                     top = fmaxf(top, x[sp].x);
                 }
-            if (top != -INFINITY)
+            if (top == -INFINITY) top = 0.f;
 #pragma unroll
-                for (int sp = 0; sp < KA_SPLITS; ++sp)
-                    if (sp < splits) {
-                        const float f = ka_exp2(x[sp].x - top);
-                        sum += f * x[sp].y;
-                        v[0] += f * y[sp].x; v[1] += f * y[sp].y; v[2] += f * y[sp].z; v[3] += f * y[sp].w;
-                    }
+            for (int sp = 0; sp < KA_SPLITS; ++sp)
+                if (sp < splits) {
+                    const float f = ka_exp2(x[sp].x - top);
+                    sum += f * x[sp].y;
+                    v[0] += f * y[sp].x; v[1] += f * y[sp].y; v[2] += f * y[sp].z; v[3] += f * y[sp].w;
+                }
         }
         if (slot >= 0) {
             float* part = a.partial + ((int64_t)slot * RT + r) * D + d;
@@ -710,10 +716,9 @@ kv4_join_kernel(const Kv4Attend a, int each) {
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
                 for (int c = c0; c <= c1; ++c) top = fmaxf(top, ml[place(c, r)].x);
-                if (top != -INFINITY) {
+                if (top == -INFINITY) top = 0.f;
 #pragma unroll 4
-                    for (int c = c0; c <= c1; ++c) add(c, r, top, sum, v);
-                }
+                for (int c = c0; c <= c1; ++c) add(c, r, top, sum, v);
                 store(r, sum, v);
             }
         return;
@@ -725,7 +730,8 @@ kv4_join_kernel(const Kv4Attend a, int each) {
         for (int k = 1; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
         float sum = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (top != -INFINITY && group < GROUPS) {
+        if (top == -INFINITY) top = 0.f;
+        if (group < GROUPS) {
 #pragma unroll 4
             for (int c = c0 + group; c <= c1; c += GROUPS) add(c, r, top, sum, v);
         }
@@ -768,8 +774,7 @@ int ka_launch(Kv4Attend a, cudaStream_t st, size_t* bytes) {
         resident[dev].store(ctas, std::memory_order_release);
     }
     constexpr int RT = 8 * NT;
-    const int64_t cap = (int64_t)a.c.table_pages << a.c.shift;
-    const int64_t keys = a.window && (int64_t)a.window + a.c.most + 15 < cap ? (int64_t)a.window + a.c.most + 15 : cap;
+    const int64_t keys = kv4_keys(a);
     a.tiles = (int)(((int64_t)a.c.most * a.group + RT - 1) / RT);
     const int64_t items = (int64_t)a.tiles * a.c.heads * a.c.sequences, units = (keys + KaDim<D, NT>::UNIT - 1) / KaDim<D, NT>::UNIT;
     const dim3 grid((unsigned)a.tiles, (unsigned)a.c.heads, (unsigned)a.c.sequences);

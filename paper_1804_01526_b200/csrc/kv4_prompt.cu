@@ -5,7 +5,8 @@
 // into swizzled shared memory, once for all rows; one thread issues S = Q K^T and O += P V; a warpgroup per row tile holds a row per thread:
 // it reads the scores from tensor memory, keeps the row's maximum and sum in FP32, and writes the probabilities back to tensor memory as the
 // bfloat16 operand of the second product (which takes it from there; V's tile is the operand with the values contiguous, keys down its rows).
-// With two row tiles the MMAs of one run while the other's softmax does; probabilities then lie in the place of their scores.
+// With two row tiles the MMAs of one run while the other's softmax does; probabilities then lie in the place of their scores. Where the row
+// tiles do not fill the GPU, the CTAs of a cluster share a tile's keys and join their results through shared memory.
 //
 // Queries and probabilities have as many bfloat16 parts as their type has bits (1, 2 or 3 as in kv4_attend.cuh), each an MMA of its own.
 // The maximum is only moved, and O rescaled, when a row's scores exceed it by more than 2^8: probabilities up to 2^8 lose nothing in FP32 and
@@ -23,6 +24,7 @@ namespace {
 
 constexpr int KP_KEYS = 128;
 constexpr float KP_SLACK = 8.0f;
+constexpr int KP_SPLITS = 8;                       // CTAs of a cluster at most
 
 template <int D, int NP> struct KpCfg {
     static constexpr int QT = NP == 1 ? 2 : 1;                             // row tiles of a CTA
@@ -35,6 +37,8 @@ template <int D, int NP> struct KpCfg {
     static constexpr int OFF_K = QT * NP * TILE, OFF_V = OFF_K + 2 * TILE, OFF_BAR = OFF_V + 2 * TILE;
     static constexpr int SMEM = 1024 + OFF_BAR + 512;
     static_assert(SMEM <= 232448, "shared memory");
+    static constexpr int OP = D + 4;                                       // FP32 of a row of a share of the keys; behind the rows their maxima and sums
+    static_assert(ROWS * (OP * 4 + 8) <= OFF_BAR, "shares");
     // columns of tensor memory
     static constexpr int S_COL = 0, O_COL = 128 * QT, P_COL = QT == 2 ? 0 : 256;     // scores and results of tile t: + 128 t; parts of P: + 64 p
 };
@@ -181,9 +185,10 @@ __device__ __forceinline__ float kp_probabilities(uint32_t sc, uint32_t pc, floa
     return s0 + s1;
 }
 
-template <int D, int NP, class T>
+// SHARE: clusters of `splits` CTAs share a row tile's keys.
+template <int D, int NP, class T, bool SHARE>
 __global__ void __launch_bounds__(KpCfg<D, NP>::THREADS, 1)
-kv4_prompt_kernel(const Kv4Attend a) {
+kv4_prompt_kernel(const Kv4Attend a, int splits) {
     using C = KpCfg<D, NP>;
     extern __shared__ unsigned char smem_dyn[];
     const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
@@ -196,7 +201,8 @@ kv4_prompt_kernel(const Kv4Attend a) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     // the tiles with the most keys first
-    const int h = blockIdx.x % a.c.heads, b = blockIdx.x / a.c.heads, tile = gridDim.y - 1 - blockIdx.y;
+    const int rank = SHARE ? blockIdx.x % splits : 0, item = SHARE ? blockIdx.x / splits : blockIdx.x;
+    const int h = item % a.c.heads, b = item / a.c.heads, tile = gridDim.y - 1 - blockIdx.y;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(kfull + 8 * i, C::FILL_WARPS);
@@ -229,7 +235,7 @@ kv4_prompt_kernel(const Kv4Attend a) {
         const int first = seq.length - seq.n;                              // position of the first query
         // keys [lo, hi): hi of the last row, lo of the first; tiles of keys for each row tile
         const int hi = max(0, min(seq.length, first + (r0 + rows - 1) / a.group + 1));
-        const int lo = a.window ? max(0, first + r0 / a.group - a.window + 1) & ~15 : 0;
+        int lo = a.window ? max(0, first + r0 / a.group - a.window + 1) & ~15 : 0;
         int n[C::QT], most = 0;
 #pragma unroll
         for (int t = 0; t < C::QT; ++t) {
@@ -237,6 +243,13 @@ kv4_prompt_kernel(const Kv4Attend a) {
             const int hi_t = 128 * t < rows ? max(0, min(seq.length, first + last / a.group + 1)) : 0;
             n[t] = hi_t > lo ? (hi_t - lo + KP_KEYS - 1) / KP_KEYS : 0;
             most = max(most, n[t]);
+        }
+        if (SHARE) {
+            const int j0 = (int)((int64_t)most * rank / splits), j1 = (int)((int64_t)most * (rank + 1) / splits);
+            lo += j0 * KP_KEYS;
+            most = j1 - j0;
+#pragma unroll
+            for (int t = 0; t < C::QT; ++t) n[t] = max(0, min(n[t] - j0, most));
         }
         const float flip = a.scale2 < 0.f ? -1.f : 1.f, scale2 = fabsf(a.scale2);
 
@@ -308,6 +321,7 @@ kv4_prompt_kernel(const Kv4Attend a) {
                 if (lane == 0) mbar_arrive(vfull + 8 * s);
                 load(a.c.v_mant, a.c.v_exps, vr, ve);
             }
+            if (SHARE) cluster_barrier();                             // as the softmax's below
         } else if (warp >= MMA_WARP) {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_MMA));
             // ------------------------------------------------------------ MMAs
@@ -365,6 +379,8 @@ kv4_prompt_kernel(const Kv4Attend a) {
                 tc_commit(done);
                 mbar_wait_soon(done, 0, abort_flag, a.c.status, 197, false);
             }
+            __syncwarp();
+            if (SHARE) cluster_barrier();
         } else {
             // ------------------------------------------------------------ softmax: a row per thread
             const int t = warp >> 2, quarter = warp & 3, r = 128 * t + quarter * 32 + lane;
@@ -423,7 +439,7 @@ kv4_prompt_kernel(const Kv4Attend a) {
             __syncwarp();
             if (lane == 0) mbar_arrive(qfull);
 
-            const int limit = r < rows ? first + own_query : first + (r0 + rows - 1) / a.group, window = a.window ? a.window : 0x7fffffff;
+            const int limit = r < rows ? first + own_query : first + (r0 + rows - 1) / a.group, window = a.window ? a.window : 1 << 30;
             // rows of this warp: the first's limit and the last's, for a look at whole tiles
             const int limit0 = __reduce_min_sync(0xffffffffu, limit), limit1 = __reduce_max_sync(0xffffffffu, limit);
             float m = -INFINITY, l = 0.f;
@@ -465,7 +481,63 @@ kv4_prompt_kernel(const Kv4Attend a) {
             }
             // ---- the row's result
             if (ok && mine > 0) ok = mbar_wait_warp_soon(odone + 8 * t, 0, abort_flag, a.c.status, 199);
-            if (ok) {
+            if constexpr (SHARE) {
+                // This CTA's share of the row to shared memory (all of the MMAs that read keys, values and queries have ended), joined with those of the
+                // cluster's other CTAs, a share of the elements by each.
+                asm volatile("bar.sync 1, %0;" ::"n"(32 * C::SOFT_WARPS) : "memory");
+                float* const os = reinterpret_cast<float*>(sm);
+                float2* const ml = reinterpret_cast<float2*>(os + C::ROWS * C::OP);
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t v[32];
+                    if (ok && mine > 0) {
+                        tc_ld32(oc + c, v);
+                        tc_wait_ld();
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = 0u;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(os + r * C::OP + c + i) = make_uint4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                }
+                ml[r] = make_float2(m, l);
+                cluster_barrier();
+                const uint32_t os_at = smem_u32(os), ml_at = smem_u32(ml);
+                const bool vec = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)((a.os.token | a.os.head) * (int64_t)sizeof(T))) & 15) == 0;
+                for (int i = rank * 32 * C::SOFT_WARPS + threadIdx.x; i < rows * (D / 4); i += splits * 32 * C::SOFT_WARPS) {
+                    const int line = i / (D / 4), d = 4 * (i - line * (D / 4));
+                    float top = -INFINITY, sum = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+                    float2 x[KP_SPLITS];
+                    float4 o[KP_SPLITS];
+#pragma unroll
+                    for (int sp = 0; sp < KP_SPLITS; ++sp)
+                        if (sp < splits) {
+                            x[sp] = ka_shared2(map_to_rank(ml_at + line * 8, sp));
+                            o[sp] = ka_shared4(map_to_rank(os_at + (line * C::OP + d) * 4, sp));
+                            top = fmaxf(top, x[sp].x);
+                        }
+                    if (top == -INFINITY) top = 0.f;
+#pragma unroll
+                    for (int sp = 0; sp < KP_SPLITS; ++sp)
+                        if (sp < splits) {
+                            const float f = ka_exp2(x[sp].x - top);
+                            sum += f * x[sp].y;
+                            y[0] += f * o[sp].x; y[1] += f * o[sp].y; y[2] += f * o[sp].z; y[3] += f * o[sp].w;
+                        }
+                    const float inv = sum > 0.f ? __frcp_rn(sum) : 0.f;    // a row that sees no key: zeros
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = sum == 0.f ? 0.f : y[e] * inv;
+                    const int query = (r0 + line) / a.group, head = h * a.group + r0 + line - query * a.group;
+                    T* const dst = reinterpret_cast<T*>(a.out) + (seq.first + query) * a.os.token + head * a.os.head + d;
+                    if (vec) {
+                        store_four(dst, y);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) dst[e] = from_f32<T>(y[e]);
+                    }
+                }
+            } else if (ok) {
                 tc_fence_after();
                 const float inv = l > 0.f ? __frcp_rn(l) : 0.f;            // a row that sees no key: zeros
                 // Through shared memory, in the place of the queries (all MMAs that read them have ended), out along the rows: 16 bytes of 32
@@ -517,18 +589,56 @@ kv4_prompt_kernel(const Kv4Attend a) {
     }
     tc_fence_before();
     __syncthreads();
+    if (SHARE && rows > 0) cluster_barrier();                         // nobody reads this CTA's share any more
     if (warp == MMA_WARP) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
     }
 }
 
+// CTAs that share the keys of a row tile: as many as the GPU has room for, where each has a tile of keys. 32 tokens of 4 x 8 heads of 128 (bfloat16)
+// behind 16384 keys 263 us with one CTA a row tile, so 43; 1024 keys 22.6 / 12.1, with two tiles of keys each at least 13.9. (A table with room for more
+// than there is: 100 keys 8.5 / 11.8.)
+template <int D, int NP, class T>
+int kp_splits(const Kv4Attend& a, int64_t tiles, int* splits) {
+    using C = KpCfg<D, NP>;
+    static std::atomic<int> resident[MAX_DEVICES][4];                      // clusters of 1, 2, 4, 8
+    const int dev = current_device();
+    if (dev < 0) return HBFP_ERR_CUDA;
+    const int64_t ctas = tiles * a.c.heads * a.c.sequences, keys = kv4_keys(a);
+    *splits = 1;
+    for (int i = 1; (1 << i) <= KP_SPLITS && keys >= (128ll << i) && (ctas << i) <= sm_count(); ++i) {
+        int room = resident[dev][i].load(std::memory_order_acquire);
+        if (!room) {
+            cudaLaunchConfig_t cfg = {};
+            cudaLaunchAttribute at[1];
+            at[0].id = cudaLaunchAttributeClusterDimension;
+            at[0].val.clusterDim.x = 1 << i; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+            cfg.gridDim = dim3(1 << i);
+            cfg.blockDim = dim3(C::THREADS);
+            cfg.dynamicSmemBytes = C::SMEM;
+            cfg.attrs = at;
+            cfg.numAttrs = 1;
+            HBFP_CUDA_OK(cudaOccupancyMaxActiveClusters(&room, kv4_prompt_kernel<D, NP, T, true>, &cfg));
+            if (room < 1) return HBFP_ERR_CUDA;
+            resident[dev][i].store(room, std::memory_order_release);
+        }
+        if (ctas > room) break;
+        *splits = 1 << i;
+    }
+    return HBFP_OK;
+}
+
 template <int D, int NP, class T>
 int kp_launch(const Kv4Attend& a, cudaStream_t st) {
     using C = KpCfg<D, NP>;
-    if (const int rc = allow_shared<kv4_prompt_kernel<D, NP, T>>(C::SMEM)) return rc;
     const int64_t rows = (int64_t)a.c.most * a.group, tiles = (rows + C::ROWS - 1) / C::ROWS;
-    launch_chained(kv4_prompt_kernel<D, NP, T>, dim3((unsigned)(a.c.heads * a.c.sequences), (unsigned)tiles), C::THREADS, C::SMEM, st, a);
+    int splits = 1;
+    int rc = allow_shared<kv4_prompt_kernel<D, NP, T, false>>(C::SMEM);
+    if (!rc) rc = allow_shared<kv4_prompt_kernel<D, NP, T, true>>(C::SMEM);
+    if (!rc) rc = kp_splits<D, NP, T>(a, tiles, &splits);
+    if (rc) return rc;
+    launch_chained_clusters(splits > 1 ? kv4_prompt_kernel<D, NP, T, true> : kv4_prompt_kernel<D, NP, T, false>, splits, dim3((unsigned)(a.c.heads * a.c.sequences * splits), (unsigned)tiles), C::THREADS, C::SMEM, st, true, a, splits);
     note_product(st);
     return launch_status();
 }
@@ -539,10 +649,18 @@ int kp_launch_dim(const Kv4Attend& a, cudaStream_t st) {
 
 }  // namespace
 
-bool kv4_prompt_eligible(const Kv4Attend& a) {
-    const int64_t rows = (int64_t)a.c.most * a.group;
-    if ((a.c.dim != 64 && a.c.dim != 128) || rows < 128 || (rows + 127) / 128 > 65535 || (int64_t)a.c.heads * a.c.sequences > (1ll << 30)) return false;
-    return true;
+// More than 32 rows, the widest tile of the kernel of few rows, which reads the keys once for each such tile but spreads any number of tiles over all
+// SMs, where a row tile here is no more than a cluster's. 32 rows take it 13 ns of an SM a key, a CTA's rows here 18 (bfloat16; binary16 19 and 24, FP32
+// 24 and 37), that is 1.4 times; up to 8192 keys it is the launch that counts, and this kernel's is one. Measured, 8 heads of 128, bfloat16, few / here:
+// 40 rows of 32 sequences with 4096 keys 179 / 145 us, of one with 4096 20.5 / 16.5, with 32768 53 / 76; 96 rows 273 / 145, 21.6 / 17.7, 74 / 77.
+bool kv4_prompt_eligible(const Kv4Attend& a, int dtype) {
+    const int64_t rows = (int64_t)a.c.most * a.group, each = dtype == HBFP_BF16 ? 256 : 128, items = (int64_t)a.c.heads * a.c.sequences;
+    if ((a.c.dim != 64 && a.c.dim != 128) || rows <= 32 || (rows + 127) / 128 > 65535 || items > (1ll << 27)) return false;
+    constexpr int64_t SMS = 148;
+    const int64_t ctas = (rows + each - 1) / each * items, waves = (ctas + SMS - 1) / SMS;
+    int splits = 1;
+    while (splits < KP_SPLITS && ctas * splits * 2 <= SMS) splits *= 2;
+    return kv4_keys(a) <= 8192 || 7 * SMS * waves <= 5 * splits * items * ((rows + 31) / 32);
 }
 
 int launch_kv4_prompt(const Kv4Attend& a, int dtype, cudaStream_t st) {

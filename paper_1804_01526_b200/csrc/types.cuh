@@ -9,11 +9,6 @@
 namespace hbfp {
 namespace {
 
-template <int DT> struct Elem;
-template <> struct Elem<HBFP_F32> { using T = float; };
-template <> struct Elem<HBFP_BF16> { using T = __nv_bfloat16; };
-template <> struct Elem<HBFP_F16> { using T = __half; };
-
 inline int64_t dtype_bytes(int dt) { return dt == HBFP_F32 ? 4 : 2; }
 inline bool dtype_ok(int dt) { return dt == HBFP_F32 || dt == HBFP_BF16 || dt == HBFP_F16; }
 
@@ -24,33 +19,6 @@ template <class T> __device__ __forceinline__ T from_f32(float x);
 template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half from_f32<__half>(float x) { return __float2half_rn(x); }
-
-// Eight neighbouring elements as FP32; p must be 16-byte aligned.
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-    const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8]) {
-    const uint4 a = __ldg(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-}
-__device__ __forceinline__ void load8(const __half* p, float (&v)[8]) {
-    const uint4 a = __ldg(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-        v[2 * i] = f.x; v[2 * i + 1] = f.y;
-    }
-}
-// The same with any alignment, elements from n on as zero.
-template <class T>
-__device__ __forceinline__ void load8_part(const T* p, int n, float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
-}
 
 // Two FP32 values as a pair of 16-bit elements (the first in the low half).
 __device__ __forceinline__ uint32_t pack_pair(float a, float b, const __nv_bfloat16*) {

@@ -707,3 +707,45 @@ def test_a_served_attention_layer(hb, dtype):
         ns = [1, 1, 1]
         lengths = [n + 1 for n in lengths]
     assert proj(o.view(3, 1, -1)).shape == (3, 1, width)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,heads,group,n", [(128, 1, 1, 128), (64, 2, 4, 100), (128, 2, 2, 200)])
+@pytest.mark.parametrize("window", [0, 2500])
+@pytest.mark.parametrize("longest", [9001, 7001])
+def test_attention_prompts_share_long_keys(hb, dtype, D, heads, group, n, window, longest):
+    """Few tiles of many rows: CTAs share a tile's keys, also where a sequence has keys for one of them only, or none."""
+    lengths = [longest, 130, n, 0, 2048 + n]
+    q, cache, table, y = check_attention(hb, dtype, heads, group, D, 64, lengths, [n, 3, n, 1, n], window=window, ragged=True)
+    again = hb.kv4_attention(q, cache, table, i32(lengths), window=window, starts=i32(np.cumsum([0, n, 3, n, 1, n]).tolist()), max_tokens=n)
+    assert torch.equal(again, y)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,heads,group,n", [(64, 2, 1, 33), (128, 1, 3, 11), (128, 2, 5, 13), (64, 1, 16, 7)])
+def test_attention_rows_between_few_and_many(hb, dtype, D, heads, group, n):
+    check_attention(hb, dtype, heads, group, D, 16, [n, 400, 1, 1500], [n] * 4)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_many_rows_of_one_head_behind_long_keys(hb, dtype, D):
+    """Tiles of many rows that a cluster each would not fill the GPU with."""
+    check_attention(hb, dtype, 1, 2, D, 64, [20000], [70])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lengths,n", [([40, 700], 2), ([9000, 5], 2), ([300, 200], 130), ([9000, 200], 130)])
+def test_attention_a_query_that_is_no_number_stays_by_itself(hb, dtype, lengths, n):
+    g = gen(3)
+    table, pages = pages_of(lengths, 64, g)
+    cache = fill(hb, g, pages, 1, 64, 128)
+    q = normal(g, 2 * n, 2, 128).to(dtype)
+    y = hb.kv4_attention(q, cache, table, i32(lengths))
+    q[1, 1, 5], q[n, 0] = math.nan, math.nan
+    z = hb.kv4_attention(q, cache, table, i32(lengths))
+    assert z[1, 1].isnan().all()
+    if lengths[1] >= n:
+        assert z[n, 0].isnan().all()
+    y[1, 1], y[n, 0], z[1, 1], z[n, 0] = 0, 0, 0, 0
+    assert torch.equal(y, z)
