@@ -947,6 +947,7 @@ PyObject* kv4_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
             out = tensor_of(a[11], "out");
             c.check_rows(out, heads, "out");
             require(out.scalar_type() == q.scalar_type() && out.size(0) == q.size(0), "out must have the type and the rows of q");
+            require((out.size(0) <= 1 || out.stride(0) > 0) && (heads <= 1 || out.stride(1) > 0), "out must have a place for every row");
         }
         const int rc = without_gil([&] {
             const c10::cuda::CUDAGuard guard(q.device());

@@ -54,7 +54,7 @@ inline int64_t kv4_keys(const Kv4Attend& a) {
 int launch_kv4_attend_f32(const Kv4Attend& a, cudaStream_t st, size_t* bytes);
 int launch_kv4_attend_bf16(const Kv4Attend& a, cudaStream_t st, size_t* bytes);
 int launch_kv4_attend_f16(const Kv4Attend& a, cudaStream_t st, size_t* bytes);
-// Many rows of a 64- or 128-wide head (kv4_prompt.cu); no workspace.
+// Many rows (kv4_prompt.cu); no workspace.
 bool kv4_prompt_eligible(const Kv4Attend& a, int dtype);
 int launch_kv4_prompt(const Kv4Attend& a, int dtype, cudaStream_t st);
 

@@ -1,7 +1,7 @@
 // Attention of many query rows (prompts) over the 4-bit cache on the fifth-generation tensor cores.
 //
-// A CTA takes 128 rows, or two tiles of 128 where a query is one bfloat16 part, of one sequence and KV head: rows = queries times the
-// query heads of the KV head. Keys come in tiles of 128. Four warps unpack a tile's keys and values to bfloat16 (exact, see kv4_attend.cuh)
+// A CTA takes 128 rows, or two tiles of 128 where a query is one bfloat16 part (of at most 128 values), of one sequence and KV head: rows = queries
+// times the query heads of the KV head. Keys come in tiles of 128 (64 of a 256-wide head). Four warps unpack a tile's keys and values to bfloat16 (exact, see kv4_attend.cuh)
 // into swizzled shared memory, once for all rows; one thread issues S = Q K^T and O += P V; a warpgroup per row tile holds a row per thread:
 // it reads the scores from tensor memory, keeps the row's maximum and sum in FP32, and writes the probabilities back to tensor memory as the
 // bfloat16 operand of the second product (which takes it from there; V's tile is the operand with the values contiguous, keys down its rows).
@@ -22,25 +22,27 @@
 namespace hbfp {
 namespace {
 
-constexpr int KP_KEYS = 128;
 constexpr float KP_SLACK = 8.0f;
 constexpr int KP_SPLITS = 8;                       // CTAs of a cluster at most
 
 template <int D, int NP> struct KpCfg {
-    static constexpr int QT = NP == 1 ? 2 : 1;                             // row tiles of a CTA
-    static constexpr int ROWS = 128 * QT, HALVES = D / 64;
+    static constexpr int QT = NP == 1 && D <= 128 ? 2 : 1;                 // row tiles of a CTA
+    static constexpr int KEYS = D <= 128 ? 128 : 64;                       // keys of a tile
+    static constexpr int STAGES = D == 256 && NP == 2 ? 1 : 2;             // tiles of keys, and of values
+    static constexpr int ROWS = 128 * QT, HALVES = (D + 63) / 64;          // (96: the last half of the second column of 64 stays unused)
     static constexpr int TILE = HALVES * 16384;                            // 128 rows of D bfloat16, 128-byte columns swizzled
+    static constexpr int COLUMN = KEYS * 128, KTILE = HALVES * COLUMN;     // the same of keys or values
     static constexpr int SOFT_WARPS = 4 * QT, FILL_WARPS = 4, THREADS = 32 * (SOFT_WARPS + FILL_WARPS + 4);      // the last four: one issues the MMAs
     // registers by role, out of what the launch has (512 x 128 or 384 x 168)
     static constexpr int REGS_SOFT = QT == 2 ? 168 : 232, REGS_FILL = QT == 2 ? 96 : 120, REGS_MMA = 56;
     static_assert(32 * (SOFT_WARPS * REGS_SOFT + FILL_WARPS * REGS_FILL + 4 * REGS_MMA) <= THREADS * (QT == 2 ? 128 : 168) - 512, "register split");
-    static constexpr int OFF_K = QT * NP * TILE, OFF_V = OFF_K + 2 * TILE, OFF_BAR = OFF_V + 2 * TILE;
+    static constexpr int OFF_K = QT * NP * TILE, OFF_V = OFF_K + STAGES * KTILE, OFF_BAR = OFF_V + STAGES * KTILE;
     static constexpr int SMEM = 1024 + OFF_BAR + 512;
     static_assert(SMEM <= 232448, "shared memory");
     static constexpr int OP = D + 4;                                       // FP32 of a row of a share of the keys; behind the rows their maxima and sums
     static_assert(ROWS * (OP * 4 + 8) <= OFF_BAR, "shares");
     // columns of tensor memory
-    static constexpr int S_COL = 0, O_COL = 128 * QT, P_COL = QT == 2 ? 0 : 256;     // scores and results of tile t: + 128 t; parts of P: + 64 p
+    static constexpr int S_COL = 0, O_COL = D == 256 ? 256 : 128 * QT, P_COL = QT == 2 ? 0 : D == 256 ? 64 : 256;     // scores and results of tile t: + 128 t; parts of P: + 64 p
 };
 
 __device__ __forceinline__ void kp_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
@@ -58,9 +60,10 @@ __device__ __forceinline__ constexpr uint32_t kp_idesc() {
     return (1u << 4) | (1u << 7) | (1u << 10) | (B_MN ? 1u << 16 : 0u) | ((uint32_t)(N >> 3) << 17) | (8u << 24);
 }
 // Descriptor of a tile whose columns are contiguous: 64 of them (128 bytes, swizzled) by 8 rows of the contraction an atom, atoms 1024 bytes
-// apart along the contraction and 16384 along the columns.
+// apart along the contraction and COLUMN along the columns.
+template <int COLUMN>
 __device__ __forceinline__ uint64_t kp_desc_mn(uint32_t addr) {
-    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(16384 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(COLUMN >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
 // One word of eight values as 16 bytes of bfloat16.
@@ -101,21 +104,22 @@ __device__ __forceinline__ float kp_max32(const uint32_t (&x)[32], float top) {
     }
     return fmaxf(top, other);
 }
+template <int KEYS>
 __device__ __forceinline__ float kp_top(uint32_t sc, const KpSight& sight, int pos, bool whole) {
     float top = -INFINITY;
     if (whole) {
         uint32_t v[2][32];
         tc_ld32(sc, v[0]);
 #pragma unroll
-        for (int c = 0; c < KP_KEYS; c += 32) {
+        for (int c = 0; c < KEYS; c += 32) {
             tc_wait_ld();
-            if (c + 32 < KP_KEYS) tc_ld32(sc + c + 32, v[(c / 32 + 1) & 1]);
+            if (c + 32 < KEYS) tc_ld32(sc + c + 32, v[(c / 32 + 1) & 1]);
             top = kp_max32(v[c / 32 & 1], top);
         }
         return top;
     }
 #pragma unroll 1
-    for (int c = 0; c < KP_KEYS; c += 32) {
+    for (int c = 0; c < KEYS; c += 32) {
         const Seen how = sight.look(pos, c);
         if (how == SEEN_NONE) continue;
         uint32_t v[32];
@@ -156,16 +160,16 @@ __device__ __forceinline__ void kp_exp32(uint32_t sc, uint32_t pc, uint64_t k2, 
 #pragma unroll
     for (int p = 0; p < NP; ++p) tc_st16(pc + 64 * p, x[p]);
 }
-template <int NP>
+template <int NP, int KEYS>
 __device__ __forceinline__ float kp_probabilities(uint32_t sc, uint32_t pc, float scale2, float m, const KpSight& sight, int pos, bool whole) {
     const uint64_t k2 = pack2(__float_as_uint(scale2), __float_as_uint(scale2)), m2 = pack2(__float_as_uint(-m), __float_as_uint(-m));
     uint64_t sum[2] = {0ull, 0ull};
     if (whole) {
 #pragma unroll
-        for (int c = 0; c < KP_KEYS; c += 32) kp_exp32<NP, false>(sc + c, pc + c / 2, k2, m2, 0u, sum);
+        for (int c = 0; c < KEYS; c += 32) kp_exp32<NP, false>(sc + c, pc + c / 2, k2, m2, 0u, sum);
     } else {
 #pragma unroll 1
-        for (int c = 0; c < KP_KEYS; c += 32) {
+        for (int c = 0; c < KEYS; c += 32) {
             const Seen how = sight.look(pos, c);
             if (how == SEEN_NONE) {
                 uint32_t zero[16];
@@ -241,12 +245,12 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
         for (int t = 0; t < C::QT; ++t) {
             const int last = min(r0 + 128 * t + 127, r0 + rows - 1);
             const int hi_t = 128 * t < rows ? max(0, min(seq.length, first + last / a.group + 1)) : 0;
-            n[t] = hi_t > lo ? (hi_t - lo + KP_KEYS - 1) / KP_KEYS : 0;
+            n[t] = hi_t > lo ? (hi_t - lo + C::KEYS - 1) / C::KEYS : 0;
             most = max(most, n[t]);
         }
         if (SHARE) {
             const int j0 = (int)((int64_t)most * rank / splits), j1 = (int)((int64_t)most * (rank + 1) / splits);
-            lo += j0 * KP_KEYS;
+            lo += j0 * C::KEYS;
             most = j1 - j0;
 #pragma unroll
             for (int t = 0; t < C::QT; ++t) n[t] = max(0, min(n[t] - j0, most));
@@ -255,18 +259,20 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
 
         if (warp >= C::SOFT_WARPS && warp < MMA_WARP) {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::REGS_FILL));
-            // ------------------------------------------------------------ unpacking: 32 keys of a tile per warp, a block of 32 values a lane and load
-            constexpr int NBLK = D / 32, KPL = 32 / NBLK, LOADS = 32 / KPL;        // blocks of a row, keys of a load, loads of 32 keys
-            const int w = warp - C::SOFT_WARPS, blk = (lane >> 3) % NBLK, sub = (lane & 7) + 8 * ((lane >> 3) / NBLK);
+            // ------------------------------------------------------------ unpacking: a quarter of a tile's keys per warp, a block of 32 values a lane and load
+            constexpr int NBLK = D / 32, WIDE = NBLK < 4 ? (NBLK + 1) / 2 * 2 : 4, TURNS = (NBLK + 3) / 4;      // blocks of a row, of it in a load, loads of a row
+            constexpr int MINE = C::KEYS / 4, KPL = 32 / WIDE, LOADS = MINE / KPL * TURNS;                    // keys of a warp, of a load; loads
+            const int w = warp - C::SOFT_WARPS, blk = (lane >> 3) % WIDE, sub = (lane & 7) + 8 * ((lane >> 3) / WIDE);
+            const bool there = NBLK % WIDE == 0 || blk < NBLK;
             uint4 kr[LOADS], vr[LOADS];
             int ke[LOADS], ve[LOADS];
-            int64_t row[2];
+            int64_t row[MINE / 16];
             int gone = 0;
             auto find = [&](int j) {
                 gone = 0;
 #pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const int p = lo + j * KP_KEYS + 32 * w + 16 * g;
+                for (int g = 0; g < MINE / 16; ++g) {
+                    const int p = lo + j * C::KEYS + MINE * w + 16 * g;
                     row[g] = -1;
                     if (j < most && p < hi) {
                         const int64_t page = kv4_page(a.c, b, p >> a.c.shift);
@@ -278,27 +284,27 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
             auto load = [&](const uint8_t* mant, const int8_t* exps, uint4 (&m)[LOADS], int (&e)[LOADS]) {
 #pragma unroll
                 for (int u = 0; u < LOADS; ++u) {
-                    const int key = KPL * u + sub;                          // of the warp's 32
-                    const int64_t at = (key >> 4) ? row[1] : row[0];
+                    const int key = KPL * (u / TURNS) + sub, block = blk + 4 * (u % TURNS);      // of the warp's
+                    const int64_t at = MINE == 16 || key < 16 ? row[0] : row[MINE / 16 - 1];
                     m[u] = make_uint4(0u, 0u, 0u, 0u);
                     e[u] = 0;
-                    if (at >= 0) {
+                    if (at >= 0 && there) {
                         const int64_t line = at + (key & 15);
-                        m[u] = __ldg(reinterpret_cast<const uint4*>(mant + line * (D / 2)) + blk);
-                        e[u] = __ldg(exps + line * NBLK + blk);
+                        m[u] = __ldg(reinterpret_cast<const uint4*>(mant + line * (D / 2)) + block);
+                        e[u] = __ldg(exps + line * NBLK + block);
                     }
                 }
             };
             auto store = [&](unsigned char* to, const uint4 (&m)[LOADS], const int (&e)[LOADS]) {
 #pragma unroll
                 for (int u = 0; u < LOADS; ++u) {
-                    const int key = 32 * w + KPL * u + sub, x = kv4_exponent((int8_t)e[u]);
+                    const int key = MINE * w + KPL * (u / TURNS) + sub, block = blk + 4 * (u % TURNS), x = kv4_exponent((int8_t)e[u]);
                     const uint32_t scale = ka_scale(x, x), offset = ka_offset(scale);
                     const uint32_t words[4] = {m[u].x, m[u].y, m[u].z, m[u].w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int c = 4 * blk + i;
-                        *reinterpret_cast<uint4*>(to + (c >> 3) * 16384 + key * 128 + (((c & 7) ^ (key & 7)) << 4)) = kp_unpack(words[i], scale, offset);
+                        const int c = 4 * block + i;
+                        if (there) *reinterpret_cast<uint4*>(to + (c >> 3) * C::COLUMN + key * 128 + (((c & 7) ^ (key & 7)) << 4)) = kp_unpack(words[i], scale, offset);
                     }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -308,16 +314,16 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
             load(a.c.k_mant, a.c.k_exps, kr, ke);
             load(a.c.v_mant, a.c.v_exps, vr, ve);
             for (int j = 0; j < most; ++j) {
-                const int s = j & 1;
-                const uint32_t ph = (uint32_t)((j >> 1) & 1) ^ 1u;
+                const int s = j % C::STAGES;
+                const uint32_t ph = (uint32_t)((j / C::STAGES) & 1) ^ 1u;
                 if (!mbar_wait_warp_soon(kempty + 8 * s, ph, abort_flag, a.c.status, 191)) break;
                 if (lane == 0) holes[(j & 3) * 4 + w] = gone;
-                store(sm + C::OFF_K + s * C::TILE, kr, ke);
+                store(sm + C::OFF_K + s * C::KTILE, kr, ke);
                 if (lane == 0) mbar_arrive(kfull + 8 * s);
                 find(j + 1);
                 load(a.c.k_mant, a.c.k_exps, kr, ke);
                 if (!mbar_wait_warp_soon(vempty + 8 * s, ph, abort_flag, a.c.status, 192)) break;
-                store(sm + C::OFF_V + s * C::TILE, vr, ve);
+                store(sm + C::OFF_V + s * C::KTILE, vr, ve);
                 if (lane == 0) mbar_arrive(vfull + 8 * s);
                 load(a.c.v_mant, a.c.v_exps, vr, ve);
             }
@@ -327,22 +333,22 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
             // ------------------------------------------------------------ MMAs
             if (warp == MMA_WARP && elect_one()) {
                 auto scores = [&](int t, int j) {
-                    const uint32_t d = tmem + C::S_COL + 128 * t, kt = base + C::OFF_K + (j & 1) * C::TILE;
+                    const uint32_t d = tmem + C::S_COL + 128 * t, kt = base + C::OFF_K + j % C::STAGES * C::KTILE;
 #pragma unroll
                     for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) {
-                            const uint32_t off = (uint32_t)(i >> 2) * 16384u + (uint32_t)(i & 3) * 32u;
-                            kp_mma(d, smem_desc_sw128(base + (t * NP + p) * C::TILE + off), smem_desc_sw128(kt + off), kp_idesc<KP_KEYS, false>(), p < NP - 1 || i > 0);
+                            const uint32_t column = (uint32_t)(i >> 2), off = (uint32_t)(i & 3) * 32u;
+                            kp_mma(d, smem_desc_sw128(base + (t * NP + p) * C::TILE + column * 16384u + off), smem_desc_sw128(kt + column * C::COLUMN + off), kp_idesc<C::KEYS, false>(), p < NP - 1 || i > 0);
                         }
                 };
                 auto values = [&](int t, int j) {
-                    const uint32_t d = tmem + C::O_COL + 128 * t, pt = tmem + C::P_COL + 128 * t, vt = base + C::OFF_V + (j & 1) * C::TILE;
+                    const uint32_t d = tmem + C::O_COL + 128 * t, pt = tmem + C::P_COL + 128 * t, vt = base + C::OFF_V + j % C::STAGES * C::KTILE;
 #pragma unroll
                     for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
-                        for (int i = 0; i < KP_KEYS / 16; ++i)
-                            kp_mma_ts(d, pt + 64 * p + 8 * i, kp_desc_mn(vt + i * 2048), kp_idesc<D, true>(), j > 0 || p < NP - 1 || i > 0);
+                        for (int i = 0; i < C::KEYS / 16; ++i)
+                            kp_mma_ts(d, pt + 64 * p + 8 * i, kp_desc_mn<C::COLUMN>(vt + i * 2048), kp_idesc<D, true>(), j > 0 || p < NP - 1 || i > 0);
                 };
                 bool ok = most == 0 || (mbar_wait_soon(qfull, 0, abort_flag, a.c.status, 189) && mbar_wait_soon(kfull, 0, abort_flag, a.c.status, 193));
                 if (ok && most > 0) {
@@ -356,9 +362,9 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
                     tc_commit(kempty);
                 }
                 for (int j = 0; ok && j < most; ++j) {
-                    const int s = j & 1, s1 = (j + 1) & 1;
-                    if (!mbar_wait_soon(vfull + 8 * s, (uint32_t)((j >> 1) & 1), abort_flag, a.c.status, 194)) { ok = false; break; }
-                    if (j + 1 < most && !mbar_wait_soon(kfull + 8 * s1, (uint32_t)(((j + 1) >> 1) & 1), abort_flag, a.c.status, 195)) { ok = false; break; }
+                    const int s = j % C::STAGES, s1 = (j + 1) % C::STAGES;
+                    if (!mbar_wait_soon(vfull + 8 * s, (uint32_t)((j / C::STAGES) & 1), abort_flag, a.c.status, 194)) { ok = false; break; }
+                    if (j + 1 < most && !mbar_wait_soon(kfull + 8 * s1, (uint32_t)(((j + 1) / C::STAGES) & 1), abort_flag, a.c.status, 195)) { ok = false; break; }
 #pragma unroll
                     for (int t = 0; t < C::QT; ++t) {
                         if (!ok || j >= n[t]) continue;
@@ -420,7 +426,7 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
                             const int line = (k0 + k) * RPL + sub;
                             const int64_t at = __shfl_sync(0xffffffffu, own_at, line);
                             e[k].zero();
-                            if (128 * t + row0 + line < rows) e[k].load(reinterpret_cast<const T*>(a.q) + at + 8 * c);
+                            if ((32 % CPR == 0 || sub < RPL) && 128 * t + row0 + line < rows) e[k].load(reinterpret_cast<const T*>(a.q) + at + 8 * c);
                         }
                     } else {
 #pragma unroll
@@ -428,11 +434,12 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
                             const int line = (k0 + k) * RPL + sub;
                             const int64_t at = __shfl_sync(0xffffffffu, own_at, line);
                             e[k].zero();
-                            if (128 * t + row0 + line < rows) e[k].load_part(reinterpret_cast<const T*>(a.q) + at + 8 * c, 8);
+                            if ((32 % CPR == 0 || sub < RPL) && 128 * t + row0 + line < rows) e[k].load_part(reinterpret_cast<const T*>(a.q) + at + 8 * c, 8);
                         }
                     }
 #pragma unroll
-                    for (int k = 0; k < UNR; ++k) put(k0 + k, e[k]);
+                    for (int k = 0; k < UNR; ++k)
+                        if (32 % CPR == 0 || sub < RPL) put(k0 + k, e[k]);
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -448,11 +455,12 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
             for (int j = 0; j < mine; ++j) {
                 if (!mbar_wait_warp_soon(sfull + 8 * t, (uint32_t)(j & 1), abort_flag, a.c.status, 198)) { ok = false; break; }
                 tc_fence_after();
-                const int pos = lo + j * KP_KEYS;
-                const int missing = holes[(j & 3) * 4] | holes[(j & 3) * 4 + 1] << 2 | holes[(j & 3) * 4 + 2] << 4 | holes[(j & 3) * 4 + 3] << 6;
+                const int pos = lo + j * C::KEYS;
+                constexpr int G = C::KEYS / 64;
+                const int missing = holes[(j & 3) * 4] | holes[(j & 3) * 4 + 1] << G | holes[(j & 3) * 4 + 2] << 2 * G | holes[(j & 3) * 4 + 3] << 3 * G;
                 const KpSight sight{limit0, limit1, limit, window, missing};
-                const bool whole = pos + KP_KEYS - 1 <= limit0 && limit1 - pos < window && missing == 0;
-                const float top = kp_top(sc, sight, pos, whole);
+                const bool whole = pos + C::KEYS - 1 <= limit0 && limit1 - pos < window && missing == 0;
+                const float top = kp_top<C::KEYS>(sc, sight, pos, whole);
                 const float top2 = top == -INFINITY ? top : top * scale2;
                 const bool move = top2 > m + KP_SLACK || (m == -INFINITY && top2 != -INFINITY);
                 if (__any_sync(0xffffffffu, move)) {
@@ -473,7 +481,7 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
                     }
                 }
                 const float m_use = m == -INFINITY ? 0.f : m;
-                l += kp_probabilities<NP>(sc, pc, scale2, m_use, sight, pos, whole);
+                l += kp_probabilities<NP, C::KEYS>(sc, pc, scale2, m_use, sight, pos, whole);
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -542,7 +550,7 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
                 const float inv = l > 0.f ? __frcp_rn(l) : 0.f;            // a row that sees no key: zeros
                 // Through shared memory, in the place of the queries (all MMAs that read them have ended), out along the rows: 16 bytes of 32
                 // rows an instruction took 2 us.
-                constexpr int V = 16 / sizeof(T), PIECES = D / V, LINE = D * (int)sizeof(T), RPS = 32 / PIECES > 0 ? 32 / PIECES : 1;
+                constexpr int V = 16 / sizeof(T), PIECES = D / V, LINE = (PIECES + 7) / 8 * 128, RPS = 32 / PIECES > 0 ? 32 / PIECES : 1;
                 unsigned char* area = sm + (t * 4 + quarter) * 32 * LINE;
 #pragma unroll
                 for (int c = 0; c < D; c += 32) {
@@ -644,23 +652,32 @@ int kp_launch(const Kv4Attend& a, cudaStream_t st) {
 }
 template <int NP, class T>
 int kp_launch_dim(const Kv4Attend& a, cudaStream_t st) {
-    return a.c.dim == 64 ? kp_launch<64, NP, T>(a, st) : kp_launch<128, NP, T>(a, st);
+    if (a.c.dim == 64) return kp_launch<64, NP, T>(a, st);
+    if (a.c.dim == 96) return kp_launch<96, NP, T>(a, st);
+    if constexpr (NP < 3)
+        if (a.c.dim == 256) return kp_launch<256, NP, T>(a, st);
+    return kp_launch<128, NP, T>(a, st);
 }
 
 }  // namespace
 
-// More than 32 rows, the widest tile of the kernel of few rows, which reads the keys once for each such tile but spreads any number of tiles over all
-// SMs, where a row tile here is no more than a cluster's. 32 rows take it 13 ns of an SM a key, a CTA's rows here 18 (bfloat16; binary16 19 and 24, FP32
-// 24 and 37), that is 1.4 times; up to 8192 keys it is the launch that counts, and this kernel's is one. Measured, 8 heads of 128, bfloat16, few / here:
-// 40 rows of 32 sequences with 4096 keys 179 / 145 us, of one with 4096 20.5 / 16.5, with 32768 53 / 76; 96 rows 273 / 145, 21.6 / 17.7, 74 / 77.
+// More rows than the widest tile of the kernel of few rows (32, of a 256-wide head 16), which reads the keys once for each such tile but spreads any
+// number of tiles over all SMs, where a row tile here is no more than a cluster's. An SM's time for a key, of such a tile there and of a CTA's rows
+// here, in ns: 128 wide 13 / 18 (bfloat16), 19 / 24 (binary16), 24 / 37 (FP32); 96 wide 13 / 19, 18 / 24, 23 / 34; 256 wide 18 / 30, 23 / 61. Up to 8192
+// keys it is the launches that count, one here. Measured, 8 heads, bfloat16, few / here: 40 rows of 128 in 32 sequences with 4096 keys 179 / 145 us, in one
+// with 4096 20.5 / 16.5, with 32768 53 / 76; 96 rows 273 / 145, 21.6 / 17.7, 74 / 77. 512 rows of 32 sequences with 2048 keys, 96 wide 641 / 167, 256 wide
+// 1813 / 422. FP32 queries of 256 have no room in shared memory.
 bool kv4_prompt_eligible(const Kv4Attend& a, int dtype) {
-    const int64_t rows = (int64_t)a.c.most * a.group, each = dtype == HBFP_BF16 ? 256 : 128, items = (int64_t)a.c.heads * a.c.sequences;
-    if ((a.c.dim != 64 && a.c.dim != 128) || rows <= 32 || (rows + 127) / 128 > 65535 || items > (1ll << 27)) return false;
+    const bool wide = a.c.dim == 256;
+    const int64_t rows = (int64_t)a.c.most * a.group, each = dtype == HBFP_BF16 && !wide ? 256 : 128, few = wide ? 16 : 32;
+    const int64_t items = (int64_t)a.c.heads * a.c.sequences;
+    if ((wide && dtype == HBFP_F32) || rows <= few || (rows + 127) / 128 > 65535 || items > (1ll << 27)) return false;
     constexpr int64_t SMS = 148;
     const int64_t ctas = (rows + each - 1) / each * items, waves = (ctas + SMS - 1) / SMS;
+    const int64_t ratio = !wide ? 14 : dtype == HBFP_BF16 ? 17 : 27;       // of the two times, in tenths
     int splits = 1;
     while (splits < KP_SPLITS && ctas * splits * 2 <= SMS) splits *= 2;
-    return kv4_keys(a) <= 8192 || 7 * SMS * waves <= 5 * splits * items * ((rows + 31) / 32);
+    return kv4_keys(a) <= (ratio < 20 ? 8192 : 1024) || ratio * SMS * waves <= 10 * splits * items * ((rows + few - 1) / few);
 }
 
 int launch_kv4_prompt(const Kv4Attend& a, int dtype, cudaStream_t st) {

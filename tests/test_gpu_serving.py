@@ -749,3 +749,38 @@ def test_attention_a_query_that_is_no_number_stays_by_itself(hb, dtype, lengths,
         assert z[n, 0].isnan().all()
     y[1, 1], y[n, 0], z[1, 1], z[n, 0] = 0, 0, 0, 0
     assert torch.equal(y, z)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,page,heads,group,n", [(96, 16, 1, 1, 130), (96, 64, 2, 3, 45), (256, 16, 1, 2, 70), (256, 64, 2, 1, 200), (256, 32, 1, 17, 1)])
+@pytest.mark.parametrize("window", [0, 1, 100])
+def test_attention_prompts_of_other_widths(hb, dtype, D, page, heads, group, n, window):
+    check_attention(hb, dtype, heads, group, D, page, [n, n + 1, n + 63, n + 500, n - 7 if n > 7 else 0], [n] * 5, window=window)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [96, 256])
+@pytest.mark.parametrize("longest", [3000, 9001])
+def test_attention_prompts_of_other_widths_share_long_keys(hb, dtype, D, longest):
+    n = 300
+    check_attention(hb, dtype, 2, 1, D, 64, [longest, 130, n, 0, 2048 + n], [n, 3, n, 1, n], window=0, ragged=True)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+def test_attention_prompts_strides_and_places(hb, dtype, D):
+    """Queries and results that are slices of wider rows, an element past a multiple of sixteen bytes."""
+    g = gen(D)
+    lengths, n = [190, 400], 90
+    table, pages = pages_of(lengths, 16, g)
+    cache = fill(hb, g, pages, 2, 16, D)
+    q = normal(g, 2 * n, 4, D).to(dtype)
+    y = hb.kv4_attention(q, cache, table, i32(lengths))
+    wide = torch.full((2 * n * 5 * D + 1,), 7.0, dtype=dtype, device="cuda")
+    out = wide[1:].view(2 * n, 5, D)[:, :4]
+    src = torch.empty(2 * n * 4 * (D + 3) + 1, dtype=dtype, device="cuda")[1:].view(2 * n, 4, D + 3)[:, :, :D]
+    src.copy_(q)
+    assert hb.kv4_attention(src, cache, table, i32(lengths), out=out) is out
+    assert torch.equal(out, y) and (wide[1:].view(2 * n, 5, D)[:, 4] == 7).all() and wide[0] == 7
+    with pytest.raises(ValueError):
+        hb.kv4_attention(q, cache, table, i32(lengths), out=torch.empty(1, 4, D, dtype=dtype, device="cuda").expand(2 * n, 4, D))
