@@ -215,20 +215,34 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
     }
     int next_id = page_of(start + (C::STAGES - 1) * C::UNIT);
     // ---- the queries, while the first keys come
-    for (int i = threadIdx.x; i < NT * C::STEPS * 32; i += KA_THREADS) {
-        const int l = i & 31, step = (i >> 5) % C::STEPS, nt = (i >> 5) / C::STEPS, r = 8 * nt + (l >> 2);
-        float e[4] = {0.f, 0.f, 0.f, 0.f};
-        if (r < rows) {
-            const int query = (r0 + r) / a.group, gh = (r0 + r) - query * a.group;
-            const T* src = reinterpret_cast<const T*>(a.q) + (seq.first + query) * a.qs.token + (h * a.group + gh) * a.qs.head + ((l & 3) * C::NB + (step >> 1)) * 8 + 4 * (step & 1);
+    const bool vec_q = ((reinterpret_cast<uintptr_t>(a.q) | (uintptr_t)((a.qs.token | a.qs.head) * (int64_t)sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
+    constexpr int QUERIES = NT * C::STEPS * 32, AHEAD = QUERIES >= 4 * KA_THREADS ? 4 : (QUERIES + KA_THREADS - 1) / KA_THREADS;      // asked for together
+#pragma unroll 1
+    for (int i0 = threadIdx.x; i0 < QUERIES; i0 += AHEAD * KA_THREADS) {
+        Four<T> e[AHEAD];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] = flip * to_f32(src[j]);
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = i0 + k * KA_THREADS, l = i & 31, step = (i >> 5) % C::STEPS, nt = (i >> 5) / C::STEPS, r = 8 * nt + (l >> 2);
+            e[k].zero();
+            if (i < QUERIES && r < rows) {
+                const int query = (r0 + r) / a.group, gh = (r0 + r) - query * a.group;
+                const T* src = reinterpret_cast<const T*>(a.q) + (seq.first + query) * a.qs.token + (h * a.group + gh) * a.qs.head + ((l & 3) * C::NB + (step >> 1)) * 8 + 4 * (step & 1);
+                if (vec_q) e[k].load(src);
+                else e[k].load_each(src);
+            }
         }
-        uint32_t x[NP], y[NP];
-        ka_parts<NP>(e[0], e[1], x);
-        ka_parts<NP>(e[2], e[3], y);
 #pragma unroll
-        for (int p = 0; p < NP; ++p) qs[p * (NT * C::STEPS * 32) + i] = make_uint2(x[p], y[p]);
+        for (int k = 0; k < AHEAD; ++k) {
+            const int i = i0 + k * KA_THREADS;
+            if (QUERIES % (AHEAD * KA_THREADS) && i >= QUERIES) break;
+            float f[4];
+            e[k].get(f);
+            uint32_t x[NP], y[NP];
+            ka_parts<NP>(flip * f[0], flip * f[1], x);
+            ka_parts<NP>(flip * f[2], flip * f[3], y);
+#pragma unroll
+            for (int p = 0; p < NP; ++p) qs[p * QUERIES + i] = make_uint2(x[p], y[p]);
+        }
     }
     // positions of this lane's rows (columns 2 t and 2 t + 1 of every eight): keys up to there are seen
     int limit[NT][2];
@@ -497,6 +511,7 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
         cluster_barrier();
     }
     const uint32_t os_at = smem_u32(os), joined_at = smem_u32(joined);
+    const bool vec_out = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)((a.os.token | a.os.head) * (int64_t)sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
     for (int i = rank * KA_THREADS + threadIdx.x; i < rows * (D / 4); i += splits * KA_THREADS) {
         const int r = i / (D / 4), d = 4 * (i - r * (D / 4));
         float top = -INFINITY, sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
@@ -531,7 +546,13 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
         const int query = (r0 + r) / a.group, gh = (r0 + r) - query * a.group;
         T* dst = reinterpret_cast<T*>(a.out) + (seq.first + query) * a.os.token + (h * a.group + gh) * a.os.head + d;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) dst[e] = from_f32<T>(v[e] * inv);
+        for (int e = 0; e < 4; ++e) v[e] *= inv;
+        if (vec_out) {
+            store_four(dst, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) dst[e] = from_f32<T>(v[e]);
+        }
     }
 }
 
@@ -793,8 +814,9 @@ int ka_launch(Kv4Attend a, cudaStream_t st, size_t* bytes) {
     }
     a.ctas = ctas;
     launch_chained(kv4_attend_split_kernel<D, NP, NT, T>, dim3((unsigned)ctas), KA_THREADS, SMEM, st, a);
-    // few tiles have many parts each: a CTA per row
-    const int each = items < 256 ? 1 : 8;
+    // Tiles of many parts each: a CTA per row. (25 sequences of 1856 keys, 28 rows of 8 heads, bfloat16: 6400 CTAs for one or two parts a tile
+    // took 26 us, 800 take 11.)
+    const int each = items * 8 <= ctas ? 1 : 8;
     launch_chained(kv4_join_kernel<D, NT, T>, dim3(grid.x * (RT / each), grid.y, grid.z), KJ_THREADS, 0, st, a, each);
     return launch_status();
 }

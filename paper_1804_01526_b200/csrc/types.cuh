@@ -123,7 +123,43 @@ struct Eight {
     }
 };
 
-// Four neighbouring elements; p must be aligned to four of them.
+// Four neighbouring elements held in their own type.
+template <class T>
+struct Four {
+    uint32_t raw[sizeof(T)];
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T); ++i) raw[i] = 0u;
+    }
+    __device__ __forceinline__ void load(const T* p) {                     // aligned to four of them
+        if constexpr (sizeof(T) == 4) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
+            raw[0] = v.x; raw[1] = v.y; raw[2] = v.z; raw[3] = v.w;
+        } else {
+            const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+            raw[0] = v.x; raw[1] = v.y;
+        }
+    }
+    __device__ __forceinline__ void load_each(const T* p) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) raw[i] = __float_as_uint(p[i]);
+        } else {
+            raw[0] = pack_pair(to_f32(p[0]), to_f32(p[1]), p);
+            raw[1] = pack_pair(to_f32(p[2]), to_f32(p[3]), p);
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[4]) const {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(raw[i]);
+        } else {
+            unpack_pair(raw[0], v[0], v[1], (const T*)nullptr);
+            unpack_pair(raw[1], v[2], v[3], (const T*)nullptr);
+        }
+    }
+};
+// They leave; p must be aligned to four of them.
 __device__ __forceinline__ void store_four(float* p, const float (&v)[4]) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
 template <class T>
 __device__ __forceinline__ void store_four(T* p, const float (&v)[4]) {
