@@ -20,10 +20,10 @@ class Int8Linear(torch.nn.Module):
     """``y = x W + b`` for inference, W ``[fin][fout]`` held as 8-bit integers; no gradients."""
 
     def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor] = None):
-        """``weight`` [fin][fout]: float32, bfloat16 or float16 on the GPU, converted here; ``bias`` [fout], kept as float32."""
+        """``weight`` [fin][fout]: float32, bfloat16 or float16 on the GPU, in any order, converted here; ``bias`` [fout], kept as float32."""
         super().__init__()
         self.fin, self.fout = weight.shape
-        rows = hb.int8_quantize(weight.detach(), 0)
+        rows = hb.int8_quantize(weight.detach().contiguous(), 0)
         self.register_buffer("weight_q", rows.q)
         self.register_buffer("weight_scale", rows.scale)
         self.register_buffer("bias", None if bias is None else bias.detach().float().contiguous())
@@ -42,6 +42,12 @@ class Int8Linear(torch.nn.Module):
         return cls(layer.weight, layer.bias)
 
     def forward(self, x: torch.Tensor) -> torch.Tensor:
-        """x [..][fin] float32, bfloat16 or float16; the result has its type. Leading extents that are one run of rows are taken as they are."""
-        y = hb.int8_gemm(x.detach().reshape(-1, self.fin), hb.Int8Rows(self.weight_q, self.weight_scale, self.fin), bias=self.bias)
+        """x [..][fin] float32, bfloat16 or float16; the result has its type. Leading extents that are one run of rows, each of
+        neighbouring values, are taken as they are; other orders (transposed, broadcast) are copied first."""
+        if x.dim() == 0 or x.shape[-1] != self.fin:
+            raise ValueError(f"x must end in an extent of {self.fin}")
+        rows = x.detach().flatten(0, -2) if x.dim() > 1 else x.detach()[None]
+        if rows.stride(1) != 1 or rows.stride(0) < self.fin:
+            rows = rows.contiguous()
+        y = hb.int8_gemm(rows, hb.Int8Rows(self.weight_q, self.weight_scale, self.fin), bias=self.bias)
         return y.view(*x.shape[:-1], self.fout)

@@ -227,6 +227,27 @@ def test_int8_linear_keeps_its_scales(hb):
     assert torch.equal(again(x), y)
 
 
+def test_int8_linear_takes_any_order(hb):
+    """Weights and tokens that are views of other tensors, transposed, broadcast or empty; a wrong extent is refused."""
+    from paper_1804_01526_b200.serving import Int8Linear
+    g = gen(6)
+    w, b = normal(g, 40, 96), normal(g, 40)
+    layer = Int8Linear(w.t(), b)
+    same = Int8Linear(w.t().contiguous(), b)
+    assert torch.equal(layer.weight_q, same.weight_q) and torch.equal(layer.weight_scale, same.weight_scale)
+    x = normal(g, 96, 5, 7)
+    for view in (x.permute(1, 2, 0), x[:, 0].t(), x[:, 0, 0], x[:, 0, :1].t().expand(4, 96), x.permute(2, 1, 0)[:, ::2], x[:1, 0, 0].expand(2, 96)):
+        y = layer(view)
+        assert y.shape == (*view.shape[:-1], 40)
+        assert torch.equal(y, layer(view.contiguous()))
+    assert layer(x.permute(1, 2, 0)[:, :0]).shape == (5, 0, 40)
+    for bad in (x.permute(1, 2, 0)[..., :48], normal(g, 4, 192), x[0, 0, 0]):
+        with pytest.raises(ValueError):
+            layer(bad)
+    nothing = Int8Linear(torch.zeros(0, 40, device="cuda"), b)
+    assert torch.equal(nothing(torch.zeros(3, 0, device="cuda")), b.expand(3, 40))
+
+
 def test_int8_gemm_of_nothing(hb):
     w = hb.int8_quantize(normal(gen(0), 8, 32))
     assert hb.int8_gemm(torch.empty(0, 32, device="cuda"), w).shape == (0, 8)
