@@ -51,10 +51,11 @@ struct Eight {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
     }
-    __device__ __forceinline__ void load_part(const T* p, int n) {         // any alignment, elements from n on zero
+    __device__ __forceinline__ void load_part(const T* p, int n) { load_between(p, 0, n); }      // any alignment, elements from n on zero
+    __device__ __forceinline__ void load_between(const T* p, int from, int n) {       // the same, and those before `from`
         T e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = i < n ? p[i] : from_f32<T>(0.f);
+        for (int i = 0; i < 8; ++i) e[i] = i >= from && i < n ? p[i] : from_f32<T>(0.f);
         uint32_t w[2 * sizeof(T)];
         if constexpr (sizeof(T) == 4) {
 #pragma unroll

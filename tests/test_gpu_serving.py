@@ -87,6 +87,24 @@ def test_int8_quantize_ties_zero_rows_and_scales_at_the_ends(hb, dtype):
     assert torch.equal(r.q[0, 1:255].int() % 2, torch.zeros(254, dtype=torch.int32, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("k", [257, 500, 1016, 1023, 1031, 1279, 1280, 4097, 5113, 9001, 10239, 16367, 16377])
+@pytest.mark.parametrize("first", [0, 1, 3, 5])
+def test_int8_quantize_rows_that_start_anywhere(hb, dtype, k, first):
+    """Rows off 16-byte borders by every number of elements, around the lengths that each number of threads holds: the result is that of a copy
+    whose rows start on borders; so are tiny rows, whose division takes another way."""
+    g = gen(k + first)
+    x = normal(g, 9, k + 7).to(dtype)
+    x[3] *= 1e-38 if dtype != torch.float16 else 1e-6
+    x[4] = 0
+    view = x[:, first:first + k]
+    place = torch.zeros(9, (k + 15) // 16 * 16, dtype=dtype, device="cuda")
+    place[:, :k] = view
+    got, want = hb.int8_quantize(view), hb.int8_quantize(place[:, :k])
+    assert torch.equal(got.scale, want.scale) and torch.equal(got.q, want.q)
+    assert not got.q[:, k:].any()
+
+
 def test_int8_quantize_views_and_out(hb):
     x = normal(gen(1), 40, 530).bfloat16()
     for v in (x[:, :512], x[:, 1:514], x[::3, 5:6], x[7:8]):
