@@ -477,6 +477,8 @@ def gemm_block_partials(a: Packed, b: Packed, impl: int = GEMM_FORCE_SIMT) -> to
 
 
 # ------------------------------------------------------------------------------ serving operators
+# None has a derivative. Under ``torch.jit.trace``, a functorch transform or a forward-mode tangent they raise RuntimeError
+# (``serving.Int8Linear`` can be traced).
 
 _DTYPE_CODES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
@@ -517,7 +519,12 @@ def int8_gemm(x, w: Int8Rows, bias: Optional[torch.Tensor] = None, out: Optional
         xq, xs = x, None
     if dtype is not None and (dtype not in _DTYPE_CODES or out is not None and out.dtype != dtype):
         raise ValueError("dtype must be float32, bfloat16 or float16, and out's where there is one")
-    return _got((_native or host()).int8_gemm(xq, xs, w.k, w.q, w.scale, bias, out, -1 if dtype is None else _DTYPE_CODES[dtype]), "hbfp_int8_gemm")
+    return _got((_native or host()).int8_gemm(xq, xs, w.k, w.q, w.scale, bias, out, -1 if dtype is None else _DTYPE_CODES[dtype], False), "hbfp_int8_gemm")
+
+
+def int8_gemm_recorded(x: torch.Tensor, w: Int8Rows, bias: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``int8_gemm`` for the forward method of an ``autograd.Function``, which is what a trace records instead of the call."""
+    return _got((_native or host()).int8_gemm(x, None, w.k, w.q, w.scale, bias, None, -1, True), "hbfp_int8_gemm")
 
 
 @dataclass

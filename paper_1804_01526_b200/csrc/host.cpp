@@ -730,12 +730,29 @@ void check_device(const at::Tensor& x, const at::Tensor& first, const char* name
 c10::DataPtr scratch(size_t bytes) {
     return bytes ? c10::cuda::CUDACachingAllocator::get()->allocate(bytes) : c10::DataPtr();
 }
+// A trace would keep the empty result and nothing that fills it, a tangent or a transform would be lost (needs_function): refused.
+// serving.Int8Linear passes through a Python function there.
+void refuse_recording(std::initializer_list<const at::Tensor*> inputs) {
+    bool refused = inputs.size() == 0 && needs_function(at::Tensor(), at::Tensor());
+    for (const at::Tensor* x : inputs) refused |= needs_function(*x, at::Tensor());
+    if (!refused) return;
+    PyErr_SetString(PyExc_RuntimeError, "serving calls cannot be recorded by a trace or transformed, and have no derivatives; call them outside, or from an autograd.Function that "
+                                        "hides them as serving.Int8Linear does");
+    throw Fail{};
+}
+
+// recorded(x) -> whether a call on x runs under something that has to see an autograd.Function
+PyObject* recorded(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (!want(n, 1)) return nullptr;
+    return layer_call([&]() -> PyObject* { return PyBool_FromLong(needs_function(tensor_of(a[0], "x"), at::Tensor())); });
+}
 
 // int8_quantize(x, axis, q or None, scale or None) -> (q, scale)
 PyObject* int8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!want(n, 4)) return nullptr;
     return guarded([&]() -> PyObject* {
         const at::Tensor x = tensor_of(a[0], "x");
+        refuse_recording({&x});
         const int dt = dtype_of(x);
         require(x.is_cuda() && dt >= 0 && x.dim() == 2 && (x.size(1) <= 1 || x.stride(1) == 1) && (x.size(0) <= 1 || x.stride(0) >= x.size(1)),
                 "x must be a 2-D float32, bfloat16 or float16 CUDA tensor with contiguous rows");
@@ -765,11 +782,13 @@ PyObject* int8_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// int8_gemm(x, x_scale or None, k, w, w_scale, bias or None, out or None, dtype of the result as in hbfp.h, -1: x's) -> out
+// int8_gemm(x, x_scale or None, k, w, w_scale, bias or None, out or None, dtype of the result as in hbfp.h, -1: x's, whether the call
+// lies in a Python function that is what a trace records) -> out
 PyObject* int8_gemm(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (!want(n, 8)) return nullptr;
+    if (!want(n, 9)) return nullptr;
     return guarded([&]() -> PyObject* {
         const at::Tensor x = tensor_of(a[0], "x"), w = tensor_of(a[3], "w"), ws = tensor_of(a[4], "w.scale");
+        if (a[8] != Py_True) refuse_recording({&x});
         const bool converted = a[1] != Py_None, fresh = a[6] == Py_None;
         const int64_t K = as_ll(a[2]), M = x.dim() == 2 ? x.size(0) : 0, N = w.dim() == 2 ? w.size(0) : 0;
         int dt = converted ? HBFP_I8 : dtype_of(x), odt = (int)as_ll(a[7]);
@@ -891,6 +910,7 @@ PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         Kv4Call c(a);
         const at::Tensor k = tensor_of(a[6], "k"), v = tensor_of(a[7], "v");
+        refuse_recording({&k, &v});
         c.check_rows(k, c.cache.heads, "k");
         c.check_rows(v, c.cache.heads, "v");
         require(k.scalar_type() == v.scalar_type() && k.size(0) == v.size(0), "k and v differ in type or tokens");
@@ -907,6 +927,7 @@ PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!want(n, 7)) return nullptr;
     return guarded([&]() -> PyObject* {
+        refuse_recording({});
         Kv4Call c(a);
         const int64_t count = as_ll(a[6]);
         require(count >= 0 && count < (1 << 30), "count is out of range");
@@ -929,6 +950,7 @@ PyObject* kv4_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         Kv4Call c(a);
         const at::Tensor q = tensor_of(a[6], "q");
+        refuse_recording({&q});
         const int64_t heads = q.dim() == 3 ? q.size(1) : 0;
         c.check_rows(q, heads, "q");
         require(heads > 0 && heads % c.cache.heads == 0, "the query heads must be a multiple of the cache's heads");
@@ -988,7 +1010,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define HBFP_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HBFP_METHOD(bind), HBFP_METHOD(packed_layout), HBFP_METHOD(quantize), HBFP_METHOD(gemm), HBFP_METHOD(gemm_q), HBFP_METHOD(wide_update),
                          HBFP_METHOD(wide_dequantize), HBFP_METHOD(conv_forward), HBFP_METHOD(conv_dgrad_filters),
-                         HBFP_METHOD(im2col_packed_t), HBFP_METHOD(linear), HBFP_METHOD(conv3x3), HBFP_METHOD(int8_quantize), HBFP_METHOD(int8_gemm),
+                         HBFP_METHOD(im2col_packed_t), HBFP_METHOD(linear), HBFP_METHOD(conv3x3), HBFP_METHOD(recorded), HBFP_METHOD(int8_quantize), HBFP_METHOD(int8_gemm),
                          HBFP_METHOD(kv4_append), HBFP_METHOD(kv4_read), HBFP_METHOD(kv4_attention),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -16,8 +16,19 @@ from . import binding as hb
 from .autograd import HbfpLinear
 
 
+class _Int8LinearFn(torch.autograd.Function):
+    """The layer as a Python function, for what has to see one: a trace records it, forward mode and transforms refuse it."""
+
+    @staticmethod
+    def forward(ctx, x, layer):
+        y = layer._product(x, hb.int8_gemm_recorded)
+        ctx.mark_non_differentiable(y)
+        return y
+
+
 class Int8Linear(torch.nn.Module):
-    """``y = x W + b`` for inference, W ``[fin][fout]`` held as 8-bit integers; no gradients."""
+    """``y = x W + b`` for inference, W ``[fin][fout]`` held as 8-bit integers; no gradients. It can be traced; the trace calls this
+    layer's product, on tokens of any number."""
 
     def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor] = None):
         """``weight`` [fin][fout]: float32, bfloat16 or float16 on the GPU, in any order, converted here; ``bias`` [fout], kept as float32."""
@@ -44,10 +55,13 @@ class Int8Linear(torch.nn.Module):
     def forward(self, x: torch.Tensor) -> torch.Tensor:
         """x [..][fin] float32, bfloat16 or float16; the result has its type. Leading extents that are one run of rows, each of
         neighbouring values, are taken as they are; other orders (transposed, broadcast) are copied first."""
+        return _Int8LinearFn.apply(x, self) if hb.host().recorded(x) else self._product(x, hb.int8_gemm)
+
+    def _product(self, x: torch.Tensor, gemm) -> torch.Tensor:
         if x.dim() == 0 or x.shape[-1] != self.fin:
             raise ValueError(f"x must end in an extent of {self.fin}")
         rows = x.detach().flatten(0, -2) if x.dim() > 1 else x.detach()[None]
         if rows.stride(1) != 1 or rows.stride(0) < self.fin:
             rows = rows.contiguous()
-        y = hb.int8_gemm(rows, hb.Int8Rows(self.weight_q, self.weight_scale, self.fin), bias=self.bias)
+        y = gemm(rows, hb.Int8Rows(self.weight_q, self.weight_scale, self.fin), bias=self.bias)
         return y.view(*x.shape[:-1], self.fout)

@@ -823,3 +823,48 @@ def test_attention_prompts_strides_and_places(hb, dtype, D):
     assert torch.equal(out, y) and (wide[1:].view(2 * n, 5, D)[:, 4] == 7).all() and wide[0] == 7
     with pytest.raises(ValueError):
         hb.kv4_attention(q, cache, table, i32(lengths), out=torch.empty(1, 4, D, dtype=dtype, device="cuda").expand(2 * n, 4, D))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_int8_linear_under_a_trace_forward_mode_and_transforms(hb, dtype):
+    """A trace records the layer and replays it on other tokens, and other numbers of them; what has no derivative of a kind says so."""
+    import torch.autograd.forward_ad as fwad
+    from paper_1804_01526_b200.serving import Int8Linear
+    g = gen(21)
+    layer = Int8Linear(normal(g, 96, 40), normal(g, 40))
+    x = normal(g, 2, 5, 96).to(dtype)
+    traced = torch.jit.trace(layer, (x,), check_trace=False)
+    for other in (x, normal(g, 2, 5, 96).to(dtype), normal(g, 7, 1, 96).to(dtype).requires_grad_(True), normal(g, 3, 2, 192).to(dtype)[..., ::2]):
+        want = layer(other)
+        got = traced(other)
+        assert torch.equal(got, want) and got.dtype == dtype and not got.requires_grad
+    with fwad.dual_level(), pytest.raises(NotImplementedError):
+        layer(fwad.make_dual(x, torch.ones_like(x)))
+    for transform in (lambda: torch.func.jvp(layer, (x,), (x,)), lambda: torch.func.grad(lambda v: layer(v).float().sum())(x), lambda: torch.func.vmap(layer)(x[None])):
+        with pytest.raises(RuntimeError, match="functorch transforms"):
+            transform()
+    assert torch.equal(layer(x), traced(x))
+
+
+def test_serving_calls_refuse_a_trace_and_tangents(hb):
+    """A trace of the calls by themselves would replay results that nothing fills."""
+    import torch.autograd.forward_ad as fwad
+    g = gen(22)
+    table, n = i32([[0, 1]]), i32([20])
+    cache, w = fill(hb, g, 2, 1, 16, 64), hb.int8_quantize(normal(g, 8, 64))
+    k = normal(g, 1, 1, 64)
+    before = [t.clone() for t in (cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps)]
+
+    def append(x):
+        hb.kv4_append(cache, x, x, table, n)
+        return x
+
+    calls = [lambda x: hb.int8_quantize(x[0]).q, lambda x: hb.int8_gemm(x[0], w), append, lambda x: hb.kv4_attention(x, cache, table, n)]
+    for call in calls + [lambda x: hb.kv4_read(cache, 1, table, n)]:
+        with pytest.raises(RuntimeError, match="trace"):
+            torch.jit.trace(call, (k,), check_trace=False)
+    for call in calls:
+        with fwad.dual_level(), pytest.raises(RuntimeError, match="derivatives"):
+            call(fwad.make_dual(k, torch.ones_like(k)))
+    assert all(torch.equal(a, b) for a, b in zip(before, (cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps)))
+    assert hb.kv4_attention(k.requires_grad_(True), cache, table, n).isfinite().all()
