@@ -400,7 +400,7 @@ HBFP_API int hbfp_gemm_block_partials(int64_t M, int64_t N, int64_t K, const hbf
  * channel of weights stored [inputs][outputs]), q is then [d1][pitch] and scale [d1]. ld = elements
  * between rows of x. pitch = bytes between rows of q: a multiple of 16, at least the contraction's
  * length; bytes behind it up to the pitch are written as zeros. q must be 16-byte aligned. A row that holds
- * an infinity or a NaN gets that as its scale (and yields infinities or NaN in products). */
+ * an infinity or a NaN gets that as its scale and zeros as its q: its products are NaN. */
 HBFP_API int hbfp_int8_quantize(const void* x, int dtype, int64_t d0, int64_t d1, int64_t ld, int contract_axis,
                                 int8_t* q, int64_t pitch, float* scale, void* stream);
 

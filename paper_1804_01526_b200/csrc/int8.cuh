@@ -18,16 +18,18 @@ struct Divider {
     float s, inv;
     bool small;              // inv is no normal number: the division is binary64's
     __device__ __forceinline__ explicit Divider(float scale) : s(scale), inv(0.f), small(false) {
-        if (!(s > 0.f) || s > 3.0e38f) s = 0.f;              // an all-zero row, or one that holds an infinity or NaN: q = 0
+        // An all-zero row, or one that holds an infinity or NaN: q = 0. (With the scale an infinity or NaN, every product of such a row is NaN.)
+        if (!(s > 0.f) || s > 3.0e38f) s = 0.f;
         else if (s < 1.0e-37f) small = true;
         else inv = __frcp_rn(s);
     }
     __device__ __forceinline__ int exactly(float x) const {
+        if (!(s > 0.f)) return 0;                            // (an infinity times 0 is no number)
         const float t = __fmaf_rn(x, inv, 12582912.0f);      // 1.5 * 2^23: rounds to the nearest whole number, halves to even
         const float r = __fmaf_rn(12582912.0f - t, s, x);
         int n = __float_as_int(t) - 0x4B400000;
         const float twice = fabsf(r) + fabsf(r);
-        if (s > 0.f && (twice > s || (twice == s && (n & 1)))) n += r > 0.f ? 1 : -1;
+        if (twice > s || (twice == s && (n & 1))) n += r > 0.f ? 1 : -1;
         return n;
     }
     // (a scale below 1e-37 is coarse: it may have been rounded down far)
@@ -53,9 +55,9 @@ struct Divider {
             unpack2(off, o0, o1);
             n[i] = __float_as_uint(t0);
             n[i + 1] = __float_as_uint(t1);
-            asm("max.f32 %0, %0, %1, %2;" : "+f"(far) : "f"(fabsf(o0)), "f"(fabsf(o1)));
+            asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(far) : "f"(fabsf(o0)), "f"(fabsf(o1)));
         }
-        if (!(far < 0.4999f)) {
+        if (!(far < 0.4999f)) {                              // next to a border, or no number
 #pragma unroll
             for (int i = 0; i < 8; ++i) n[i] = (uint32_t)exactly(x[i]);
         }

@@ -868,3 +868,34 @@ def test_serving_calls_refuse_a_trace_and_tangents(hb):
             call(fwad.make_dual(k, torch.ones_like(k)))
     assert all(torch.equal(a, b) for a, b in zip(before, (cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps)))
     assert hb.kv4_attention(k.requires_grad_(True), cache, table, n).isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,K,first", [(2, 300, 0), (3, 4096, 0), (3, 523, 1), (40, 300, 0), (5, 9001, 3), (200, 77, 0), (2100, 1024, 0)])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_int8_rows_that_hold_no_finite_number_are_nan(hb, dtype, M, K, first, bad):
+    """Whatever the sign, the place and the kernel: q is 0 there, the row's scale is the infinity or NaN, and 0 times it is NaN in every result."""
+    g = gen(K + M)
+    x = normal(g, M, K + 8).to(dtype)[:, first:first + K]
+    rows = sorted({0, 1, M - 1})
+    for i, r in enumerate(rows):
+        x[r, (K - 1) * i // max(len(rows) - 1, 1)] = bad
+    w = hb.int8_quantize(normal(g, 3000 if M > 1000 else 24, K))
+    q = hb.int8_quantize(x)
+    assert not q.q[rows].any() and not q.scale[rows].isfinite().any()
+    for y in (hb.int8_gemm(x, w), hb.int8_gemm(q, w, dtype=dtype)):
+        assert y[rows].isnan().all()
+        clean = torch.ones(M, dtype=torch.bool, device="cuda")
+        clean[rows] = False
+        assert y[clean].isfinite().all()
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_int8_channels_that_hold_no_finite_number_are_nan(hb, bad):
+    g = gen(31)
+    w = normal(g, 300, 70)
+    w[17, 3] = bad
+    q = hb.int8_quantize(w, 0)
+    assert not q.q[3].any() and not q.scale[3].isfinite()
+    y = hb.int8_gemm(normal(g, 5, 300), q)
+    assert y[:, 3].isnan().all() and y.isnan().sum() == 5
