@@ -242,7 +242,7 @@ __device__ __forceinline__ void int8_send_box(const Int8Out& out, unsigned char*
         __syncwarp();
         if (lane == 0 && row0 < out.M && col0 < out.N) {
             asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
-                         ::"l"(reinterpret_cast<uint64_t>(out.map)), "r"(smem_u32(box)), "r"(col0 * (int)sizeof(T)), "r"(row0) : "memory");
+                         ::"l"(reinterpret_cast<uint64_t>(out.map)), "r"(smem_u32(box)), "r"(col0), "r"(row0) : "memory");
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
         }
         return;
@@ -603,12 +603,13 @@ int quantize_any(const T* x, int64_t d0, int64_t d1, int64_t ld, int axis, int8_
     return launch_status();
 }
 
-// Tensor map of the result in boxes of 32 rows x 128 bytes, where its pitch and place allow one.
+// Tensor map of the result in boxes of 32 rows x 128 bytes, where its pitch and place allow one. It counts elements: a column's byte can lie
+// past 2^31, where the copy engine's coordinates end.
 template <class T>
 int map_result(Int8Problem& p, CUtensorMap* m) {
     p.tma_out = p.ldy * (int64_t)sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(p.y) & 15) == 0;
     if (!p.tma_out) { *m = CUtensorMap{}; return HBFP_OK; }
-    return make_map(m, p.y, (uint64_t)p.N * sizeof(T), p.M, p.ldy * sizeof(T), 128, 32, true);
+    return make_map(m, p.y, p.N, p.M, p.ldy * sizeof(T), 128 / sizeof(T), 32, true, sizeof(T) == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16);
 }
 
 template <class T, int NT>

@@ -364,16 +364,17 @@ EncodeTiledFn encode_fn() {
     return fn;
 }
 
-// 2-D byte tensor [outer][inner] with row pitch `pitch`; box {box_inner, box_outer}.
+// 2-D tensor [outer][inner] with row pitch `pitch` in bytes; box {box_inner, box_outer}. Extents and coordinates along the rows count
+// elements of `type`, bytes unless given.
 int make_map(CUtensorMap* m, const void* ptr, uint64_t inner, uint64_t outer, uint64_t pitch, uint32_t box_inner,
-             uint32_t box_outer, bool swizzle128) {
+             uint32_t box_outer, bool swizzle128, CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_UINT8) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return HBFP_ERR_CUDA;
     cuuint64_t dims[2] = {inner, outer};
     cuuint64_t strides[1] = {pitch};
     cuuint32_t box[2] = {box_inner, box_outer};
     cuuint32_t estr[2] = {1, 1};
-    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(ptr), dims, strides, box, estr,
+    CUresult r = fn(m, type, 2, const_cast<void*>(ptr), dims, strides, box, estr,
                     CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? HBFP_OK : HBFP_ERR_CUDA;

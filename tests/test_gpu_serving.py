@@ -899,3 +899,27 @@ def test_int8_channels_that_hold_no_finite_number_are_nan(hb, bad):
     assert not q.q[3].any() and not q.scale[3].isfinite()
     y = hb.int8_gemm(normal(g, 5, 300), q)
     assert y[:, 3].isnan().all() and y.isnan().sum() == 5
+
+
+def test_int8_gemm_columns_past_two_gigabytes_of_a_row(hb):
+    """A row of results longer than 2^31 bytes: the columns behind are those of the same channels by themselves."""
+    N, K, M = (1 << 29) + 100, 16, 5
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 28 << 30:
+        pytest.skip("not enough device memory")
+    g = gen(41)
+    w = hb.Int8Rows(torch.zeros(N, K, dtype=torch.int8, device="cuda"), torch.ones(N, device="cuda"), K)
+    parts = [slice(0, 300), slice((1 << 29) - 130, (1 << 29) + 10), slice(N - 77, N)]
+    for p in parts:
+        w.q[p] = torch.randint(-127, 128, (p.stop - p.start, K), dtype=torch.int8, device="cuda", generator=g)
+        w.scale[p] = normal(g, p.stop - p.start).abs()
+    x = normal(g, M, K)
+    y = hb.int8_gemm(x, w)
+    for p in parts:
+        some = hb.Int8Rows(w.q[p].contiguous(), w.scale[p].contiguous(), K)
+        check_product(hb, x, some, None, y[:, p])
+        assert torch.equal(y[:, p], hb.int8_gemm(x, some))
+        y[:, p] = 0
+    assert all(not y[:, i:i + (1 << 27)].any() for i in range(0, N, 1 << 27))
+    del w, x, y
+    torch.cuda.empty_cache()
