@@ -465,8 +465,8 @@ HBFP_API int hbfp_kv4_read(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* ba
 
 /* out[row][head] = sum_j p_j v_j with p = softmax_j(scale * q[row][head] . k_j) over the positions j <= own position
  * (and > own position - window where window > 0) of the row's sequence. q and out [tokens][heads*group][dim] (element strides,
- * dim contiguous); query head i reads KV head i / group. A row that sees no key is zeros. Append the call's own keys first. The
- * workspace (256-byte aligned) takes the parts of a sequence that several CTAs share. */
+ * dim contiguous); query head i reads KV head i / group. scale * log2(e) must be finite in FP32. A row that sees no key is zeros. Append the
+ * call's own keys first. The workspace (256-byte aligned) takes the parts of a sequence that several CTAs share. */
 HBFP_API int hbfp_kv4_attention_workspace(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int dtype, int32_t group,
                                           int32_t window, size_t* bytes);
 HBFP_API int hbfp_kv4_attention(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int dtype, const void* q, int64_t q_token,

@@ -567,7 +567,7 @@ def kv4_attention(q: torch.Tensor, cache: Kv4Cache, page_table: torch.Tensor, le
                   window: int = 0, starts: Optional[torch.Tensor] = None, max_tokens: Optional[int] = None,
                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """hbfp_kv4_attention: causal attention of ``q [tokens][heads * group][dim]`` (any strides of tokens and heads) over the cache,
-    the last ``window`` positions of it where that is not 0; ``scale`` is 1 / sqrt(dim) unless given. Tokens, ``page_table``, ``lengths``, ``starts`` and
+    the last ``window`` positions of it where that is not 0; ``scale`` (finite) is 1 / sqrt(dim) unless given. Tokens, ``page_table``, ``lengths``, ``starts`` and
     ``max_tokens`` as in ``kv4_append``, which writes the call's own keys and values first. A row that sees no key is zeros; rows behind the last sequence's are
     left as they are (not set in a new result)."""
     return _got((_native or host()).kv4_attention(cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps, page_table, lengths, q, scale, window, starts,

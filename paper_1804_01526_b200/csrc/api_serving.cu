@@ -1,4 +1,6 @@
 // extern "C" entry points of the serving operators: argument checks, workspace, dispatch.
+#include <cmath>
+
 #include "kv4_attend.cuh"
 
 namespace hbfp {
@@ -17,6 +19,7 @@ int launch_kv4_read(const Kv4Args& a, int count, float* k, float* v, cudaStream_
 namespace {
 
 constexpr int64_t INT8_MOST_K = 131072;              // 128 * 128 * K fits int32
+constexpr float LOG2_E = 1.4426950408889634f;
 constexpr int64_t MOST = 1ll << 30;                  // extents the kernels index with 32 bits
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -167,6 +170,7 @@ int hbfp_kv4_attention(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch,
                        float scale, int32_t window, void* out, int64_t out_token, int64_t out_head, void* workspace, size_t workspace_bytes, void* stream) {
     size_t need = 0;
     Kv4Attend a{};
+    if (!std::isfinite(scale * LOG2_E)) return HBFP_ERR_INVALID_ARG;       // (the kernels would not agree on what it gives)
     if (const int rc = attend(cache, batch, dtype, group, window, &a, nullptr, &need)) return rc;
     if (a.c.sequences == 0 || a.c.most == 0 || a.c.tokens == 0) return HBFP_OK;
     if (!q || !out) return HBFP_ERR_INVALID_ARG;
@@ -176,7 +180,7 @@ int hbfp_kv4_attention(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch,
     a.qs = Kv4Rows{q_token, q_head};
     a.out = out;
     a.os = Kv4Rows{out_token, out_head};
-    a.scale2 = scale * 1.4426950408889634f;
+    a.scale2 = scale * LOG2_E;
     a.partial = static_cast<float*>(workspace);
     return attend(cache, batch, dtype, group, window, &a, static_cast<cudaStream_t>(stream), nullptr);
 }

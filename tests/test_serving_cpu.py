@@ -141,3 +141,16 @@ def test_binding_refuses_what_it_can_see(hb):
 
 def test_status_of_index_errors_has_a_text(hb):
     assert "out of range" in hb.status_string(hb.ERR_INDEX)
+
+
+def test_attention_refuses_a_scale_that_is_no_number(hb):
+    """Also one whose product with log2(e) is none. Nothing else is wrong with the calls: without a sequence they have nothing to do."""
+    c, b = ctypes.byref(cache()), ctypes.byref(batch(sequences=0, tokens=0))
+
+    def go(scale):
+        return hb.lib().hbfp_kv4_attention(c, b, 0, None, 128, 64, 1, scale, 0, None, 128, 64, None, 0, None)
+
+    for scale in (float("nan"), float("inf"), -float("inf"), 3.0e38, -3.0e38):
+        assert go(scale) == hb.ERR_INVALID_ARG, scale
+    for scale in (0.0, -2.0, 1e-45, 2.3e38):
+        assert go(scale) == hb.OK, scale
