@@ -170,7 +170,7 @@ __device__ __forceinline__ void ka_tile(const Kv4Attend& a, int b, const Kv4Seq&
     constexpr int RT = 8 * NT, MT = C::CH / 16, TILES = 4 * C::VW;        // TILES: 16-row tiles of V^T
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int rows = min(RT, seq.n * a.group - tile * RT), r0 = tile * RT;
-    const float flip = a.scale2 < 0.f ? -1.f : 1.f, scale2 = fmaxf(fabsf(a.scale2), 1e-37f);      // a negative scale is a negative query; 0 times an unseen -inf would be NaN
+    const float flip = a.scale2 < 0.f ? -1.f : 1.f, scale2 = fmaxf(fabsf(a.scale2), 1.4e-45f);      // a negative scale is a negative query; 0 times an unseen -inf would be NaN
     uint2* qs = reinterpret_cast<uint2*>(sm);                             // [NP][NT][STEPS][32]
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");          // (copies follow where results were written)
     __syncthreads();                                                      // the tile before is through with shared memory

@@ -923,3 +923,23 @@ def test_int8_gemm_columns_past_two_gigabytes_of_a_row(hb):
     assert all(not y[:, i:i + (1 << 27)].any() for i in range(0, N, 1 << 27))
     del w, x, y
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows", [1, 40])
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-42])
+def test_attention_scales_near_zero_and_keys_of_the_largest_size(hb, dtype, rows, scale):
+    """Scores of 1e37 times nothing, or times next to nothing (1e-5), weigh all keys alike: the average of the values, to FP32's accuracy for the
+    sums and the type's for probabilities and result, whatever the number of rows."""
+    g = gen(51)
+    cache, n = hb.kv4_alloc(2, 1, 16, 64), 32
+    k, v = torch.zeros(n, 1, 64, device="cuda"), normal(g, n, 1, 64)
+    k[::3, 0, 5] = 2.0 ** 120
+    table, lengths = i32([[0, 1]]), i32([n])
+    hb.kv4_append(cache, k, v, table, lengths)
+    q = torch.full((rows, 1, 64), 10.0, device="cuda", dtype=dtype)
+    y = hb.kv4_attention(q, cache, table, lengths, scale=scale)
+    V = unpack(cache.v_mant, cache.v_exps).transpose(1, 2).flatten(0, 1)[:, 0]
+    for i in range(max(0, rows - n), rows):
+        seen = V[:n - rows + i + 1]
+        assert (y[i, 0].double() - seen.mean(0)).abs().le(3e-5 * seen.abs().mean(0) + 2 * u(dtype) * seen.abs().mean(0) + 1e-30).all()
