@@ -852,7 +852,7 @@ struct Kv4Call {
             require(arrays[i].size(3) * (i & 1 ? 16 : 1) == arrays[0].size(3), "the cache's arrays differ in width");
         }
         const at::Tensor& m = arrays[0];
-        require(m.size(1) < (1 << 30) && m.size(2) < (1 << 30) && m.size(3) < (1 << 28), "the cache's extents are out of range");
+        require(m.size(1) >= 1 && m.size(1) < (1 << 30) && m.size(2) < (1 << 30) && m.size(3) < (1 << 28), "the cache's extents are out of range");
         cache.struct_size = sizeof(cache);
         cache.pages = m.size(0);
         cache.heads = (int32_t)m.size(1);

@@ -943,3 +943,13 @@ def test_attention_scales_near_zero_and_keys_of_the_largest_size(hb, dtype, rows
     for i in range(max(0, rows - n), rows):
         seen = V[:n - rows + i + 1]
         assert (y[i, 0].double() - seen.mean(0)).abs().le(3e-5 * seen.abs().mean(0) + 2 * u(dtype) * seen.abs().mean(0) + 1e-30).all()
+
+
+def test_a_cache_without_heads_is_refused(hb):
+    """(The query heads are counted in heads of the cache.)"""
+    cache = hb.Kv4Cache(*(torch.empty(2, 0, 16, w, dtype=t, device="cuda") for w, t in ((32, torch.uint8), (2, torch.int8)) * 2))
+    table, n = i32([[0, 1]]), i32([3])
+    for call in (lambda: hb.kv4_attention(normal(gen(0), 1, 2, 64), cache, table, n), lambda: hb.kv4_read(cache, 1, table, n),
+                 lambda: hb.kv4_append(cache, torch.empty(1, 0, 64, device="cuda"), torch.empty(1, 0, 64, device="cuda"), table, n)):
+        with pytest.raises(ValueError, match="extents"):
+            call()
