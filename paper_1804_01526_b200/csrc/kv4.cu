@@ -31,7 +31,7 @@ struct Kv4Words {
 // Row of the cache's arrays for a head of the token t of the sequence's new ones; -1: it has no place.
 __device__ __forceinline__ int64_t kv4_row(const Kv4Args& a, int b, const Kv4Seq& s, int64_t t, int head) {
     const int64_t p = (int64_t)s.length - s.n + t;
-    if (t >= s.n || p < 0 || p >= s.length) return -1;
+    if (t >= s.n || p < 0 || p >= s.held) return -1;
     const int64_t page = kv4_page(a, b, (int)p >> a.shift);
     return page < 0 ? -1 : ((page * a.heads + head) << a.shift) + ((int)p & (a.page - 1));
 }

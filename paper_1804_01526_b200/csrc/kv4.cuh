@@ -40,11 +40,12 @@ namespace {
 struct Kv4Seq {
     int64_t first;      // its first row among the call's tokens
     int n, length;      // tokens of this call, tokens in the cache when they are in it
+    int held;           // those of them that the page table has room for: the rest has no place, its positions stay what they are
     bool bad;           // one of the numbers was out of range
 };
 
-// The numbers come from the caller's device memory: whatever they are, a row lies within the call's tokens and a position within the table. (Not
-// reported here: a branch on the length would keep loads that do not need it waiting.)
+// The numbers come from the caller's device memory: whatever they are, a row lies within the call's tokens and a position below `held` within
+// the table. (Not reported here: a branch on the length would keep loads that do not need it waiting.)
 __device__ __forceinline__ Kv4Seq kv4_seq_unreported(const Kv4Args& a, int b) {
     Kv4Seq s;
     bool bad = false;
@@ -58,11 +59,12 @@ __device__ __forceinline__ Kv4Seq kv4_seq_unreported(const Kv4Args& a, int b) {
         s.n = a.most;
         s.first = (int64_t)b * a.most;
     }
-    const int64_t cap = (int64_t)a.table_pages << a.shift;
+    const int cap = (int)((int64_t)a.table_pages << a.shift);             // (below 2^30)
     const int len = __ldg(a.lengths + b);
     s.length = len < 0 ? 0 : len;
-    if (s.length > cap) { bad = true; s.length = (int)cap; }
-    s.bad = bad;
+    if (len >= 1 << 30) { s.length = 0; s.n = 0; }                        // positions have 30 bits: all of the sequence is left out
+    s.held = min(s.length, cap);
+    s.bad = bad || len > cap;
     return s;
 }
 __device__ __forceinline__ void kv4_report(const Kv4Args& a, const Kv4Seq& s) {
@@ -74,7 +76,7 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Args& a, int b) {
     return s;
 }
 
-// The page that holds position p (0 <= p < length) of sequence b; -1 for a number that is no page of the cache.
+// The page that holds position p (0 <= p < held) of sequence b; -1 for a number that is no page of the cache.
 __device__ __forceinline__ int64_t kv4_page(const Kv4Args& a, int b, int index) {
     const int id = __ldg(a.table + (int64_t)b * a.table_ld + index);
     if (id < 0 || id >= a.pages) {

@@ -575,7 +575,7 @@ __device__ __forceinline__ KaRing ka_ring(unsigned char* sm) {
 __device__ __forceinline__ KaRange ka_range(const Kv4Attend& a, const Kv4Seq& s, int first_query, int last_query) {
     KaRange r;
     const int base = s.length - s.n;
-    r.hi = max(0, min(s.length, base + last_query + 1));
+    r.hi = max(0, min(s.held, base + last_query + 1));
     r.lo = a.window ? max(0, base + first_query - a.window + 1) & ~63 : 0;
     return r;
 }

@@ -238,13 +238,13 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
     if (rows > 0) {
         const int first = seq.length - seq.n;                              // position of the first query
         // keys [lo, hi): hi of the last row, lo of the first; tiles of keys for each row tile
-        const int hi = max(0, min(seq.length, first + (r0 + rows - 1) / a.group + 1));
+        const int hi = max(0, min(seq.held, first + (r0 + rows - 1) / a.group + 1));
         int lo = a.window ? max(0, first + r0 / a.group - a.window + 1) & ~15 : 0;
         int n[C::QT], most = 0;
 #pragma unroll
         for (int t = 0; t < C::QT; ++t) {
             const int last = min(r0 + 128 * t + 127, r0 + rows - 1);
-            const int hi_t = 128 * t < rows ? max(0, min(seq.length, first + last / a.group + 1)) : 0;
+            const int hi_t = 128 * t < rows ? max(0, min(seq.held, first + last / a.group + 1)) : 0;
             n[t] = hi_t > lo ? (hi_t - lo + C::KEYS - 1) / C::KEYS : 0;
             most = max(most, n[t]);
         }
@@ -277,8 +277,8 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
                     if (j < most && p < hi) {
                         const int64_t page = kv4_page(a.c, b, p >> a.c.shift);
                         if (page >= 0) row[g] = ((page * a.c.heads + h) << a.c.shift) + (p & (a.c.page - 1));
-                        else gone |= 1 << g;
                     }
+                    if (row[g] < 0) gone |= 1 << g;                          // (behind hi too: a row's own position can lie behind the page table)
                 }
             };
             auto load = [&](const uint8_t* mant, const int8_t* exps, uint4 (&m)[LOADS], int (&e)[LOADS]) {

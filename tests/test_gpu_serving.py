@@ -953,3 +953,79 @@ def test_a_cache_without_heads_is_refused(hb):
                  lambda: hb.kv4_append(cache, torch.empty(1, 0, 64, device="cuda"), torch.empty(1, 0, 64, device="cuda"), table, n)):
         with pytest.raises(ValueError, match="extents"):
             call()
+
+
+@pytest.mark.parametrize("length,n", [(50, 5), (48 + 70, 70), (49, 49), (200, 3)])
+def test_positions_behind_the_page_table_are_left_out(hb, length, n):
+    """A sequence longer than its table of 48: new tokens that have a place go there, the rest nowhere, and nothing else is touched. The other
+    sequence is written as ever."""
+    g = gen(length)
+    cache = fill(hb, g, 5, 2, 16, 64)
+    arrays = (cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps)
+    old = [t.clone() for t in arrays]
+    k, v = normal(g, n + 1, 2, 64), normal(g, n + 1, 2, 64)
+    table, starts = i32([[3, 0, 4], [1, -1, -1]]), i32([0, n, n + 1])
+    hb.kv4_append(cache, k, v, table, i32([length, 7]), starts=starts)
+    assert hb.device_status_rc() == (hb.ERR_INDEX, 1002)
+    want = hb.Kv4Cache(*(t.clone() for t in old))
+    there = max(0, min(n, 48 - (length - n)))
+    if there:
+        hb.kv4_append(want, k[:there], v[:there], table[:1], i32([length - n + there]))
+    hb.kv4_append(want, k[n:], v[n:], table[1:], i32([7]))
+    assert hb.device_status() == 0
+    assert all(torch.equal(a, b) for a, b in zip(arrays, (want.k_mant, want.k_exps, want.v_mant, want.v_exps)))
+    rk, rv = hb.kv4_read(cache, n, table[:1], i32([length]))
+    assert hb.device_status_rc() == (hb.ERR_INDEX, 1002)
+    assert not rk[there:].any() and not rv[there:].any()
+    if there:
+        ek, ev = hb.kv4_read(cache, there, table[:1], i32([length - n + there]))
+        assert torch.equal(rk[:there], ek) and torch.equal(rv[:there], ev)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("pages,length,n", [(3, 50, 5), (3, 48 + 70, 70), (3, 49, 1), (300, 4990, 1), (300, 4990, 200), (5, 81, 40), (3, 4000, 2)])
+@pytest.mark.parametrize("window", [0, 30])
+def test_attention_behind_the_page_table(hb, dtype, D, pages, length, n, window):
+    """Rows of a sequence longer than its table see what the table holds of the keys up to their own positions: the definition in 64 bits, and the
+    bound of attend_reference with that many keys."""
+    g = gen(length + n + D)
+    cap = 16 * pages
+    cache = fill(hb, g, pages, 1, 16, D)
+    table = torch.randperm(pages, generator=g, device="cuda").int()[None]
+    q = normal(g, n, 2, D).to(dtype)
+    y = hb.kv4_attention(q, cache, table, i32([length]), window=window)
+    assert hb.device_status_rc() == (hb.ERR_INDEX, 1002)
+    K, V = (unpack(m, e)[table[0].long()].transpose(0, 1).flatten(1, 2)[0] for m, e in ((cache.k_mant, cache.k_exps), (cache.v_mant, cache.v_exps)))
+    i, j = torch.arange(length - n, length, device="cuda")[:, None], torch.arange(cap, device="cuda")[None]
+    seen = (j <= i) & (j > i - window if window else j >= 0)
+    parts = {torch.bfloat16: 1, torch.float16: 2, torch.float32: 3}[dtype]
+    for h in range(2):
+        x = q[:, h].double()
+        s = (x @ K.t() * D ** -0.5).masked_fill(~seen, -math.inf)
+        p = torch.where(seen.any(-1, keepdim=True), torch.softmax(s, -1), 0.0)
+        ref = p @ V
+        S = (x.abs() @ K.abs().t() * D ** -0.5).masked_fill(~seen, 0.0).max(-1, keepdim=True).values
+        err = 2 * S * ((parts * D / 16 + 8) * 2.0 ** -22) + 2.0 ** -20 + (cap / 16 + 8) * 2.0 ** -22 + u(torch.bfloat16) ** parts
+        tol = (p @ V.abs()) * err + u(dtype) * ref.abs() + (2.0 ** -25 if dtype == torch.float16 else 1e-40)
+        assert (y[:, h].double() - ref).abs().le(tol).all(), ((y[:, h].double() - ref).abs() / tol).max()
+
+
+def test_sequences_of_more_tokens_than_positions_have_bits_are_left_out(hb):
+    g = gen(61)
+    cache = fill(hb, g, 3, 1, 16, 64)
+    arrays = (cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps)
+    old = [t.clone() for t in arrays]
+    table, k = i32([[0, 1, 2]] * 2), normal(g, 2, 1, 64)
+    good = hb.kv4_attention(k, cache, table, i32([20, 40]))
+    for length in (1 << 30, 2 ** 31 - 1):
+        hb.kv4_append(cache, k[:1], k[:1], table[:1], i32([length]))
+        assert hb.device_status_rc() == (hb.ERR_INDEX, 1002)
+        y = hb.kv4_attention(k, cache, table, i32([length, 40]), out=torch.full_like(k, 3.0))
+        assert hb.device_status_rc() == (hb.ERR_INDEX, 1002)
+        assert (y[0] == 3.0).all() and torch.equal(y[1], good[1])
+        many = hb.kv4_attention(normal(g, 200, 1, 64), cache, table[:1], i32([length]), window=2 ** 31 - 1, out=torch.full((200, 1, 64), 3.0, device="cuda"))
+        assert hb.device_status_rc() == (hb.ERR_INDEX, 1002) and (many == 3.0).all()
+    many = hb.kv4_attention(normal(g, 200, 1, 64), cache, table[:1], i32([(1 << 30) - 1]))
+    assert hb.device_status_rc() == (hb.ERR_INDEX, 1002) and many.isfinite().all() and many.any()
+    assert all(torch.equal(a, b) for a, b in zip(arrays, old))
