@@ -277,8 +277,10 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
                     if (j < most && p < hi) {
                         const int64_t page = kv4_page(a.c, b, p >> a.c.shift);
                         if (page >= 0) row[g] = ((page * a.c.heads + h) << a.c.shift) + (p & (a.c.page - 1));
+                        else gone |= 1 << g;
+                    } else {                                                 // behind hi, where a row's own position can lie (a length beyond the page table);
+                        gone |= 1 << g;                                      // (one test for both cases: other registers, 2 x 2048 tokens 180 -> 184 us)
                     }
-                    if (row[g] < 0) gone |= 1 << g;                          // (behind hi too: a row's own position can lie behind the page table)
                 }
             };
             auto load = [&](const uint8_t* mant, const int8_t* exps, uint4 (&m)[LOADS], int (&e)[LOADS]) {
