@@ -504,9 +504,9 @@ bool has_tangent(const at::Tensor& t) {
     const torch::autograd::AutogradMeta* meta = t.defined() ? torch::autograd::impl::get_autograd_meta(t) : nullptr;
     return meta && meta->fw_grad_ && t._fw_grad(/*level=*/0).defined();
 }
+bool calls_are_seen() { return torch::jit::tracer::isTracing() || c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode); }
 bool needs_function(const at::Tensor& x, const at::Tensor& weight, const at::Tensor& bias = at::Tensor()) {
-    return torch::jit::tracer::isTracing() || c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode) ||
-           has_tangent(x) || has_tangent(weight) || has_tangent(bias);
+    return calls_are_seen() || has_tangent(x) || has_tangent(weight) || has_tangent(bias);
 }
 // Everything a pass computes lies below autograd; gradients come out as plain tensors.
 struct Below {
@@ -733,8 +733,8 @@ c10::DataPtr scratch(size_t bytes) {
 // A trace would keep the empty result and nothing that fills it, a tangent or a transform would be lost (needs_function): refused.
 // serving.Int8Linear passes through a Python function there.
 void refuse_recording(std::initializer_list<const at::Tensor*> inputs) {
-    bool refused = inputs.size() == 0 && needs_function(at::Tensor(), at::Tensor());
-    for (const at::Tensor* x : inputs) refused |= needs_function(*x, at::Tensor());
+    bool refused = calls_are_seen();
+    for (const at::Tensor* x : inputs) refused |= has_tangent(*x);
     if (!refused) return;
     PyErr_SetString(PyExc_RuntimeError, "serving calls cannot be recorded by a trace or transformed, and have no derivatives; call them outside, or from an autograd.Function that "
                                         "hides them as serving.Int8Linear does");
@@ -744,7 +744,7 @@ void refuse_recording(std::initializer_list<const at::Tensor*> inputs) {
 // recorded(x) -> whether a call on x runs under something that has to see an autograd.Function
 PyObject* recorded(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!want(n, 1)) return nullptr;
-    return layer_call([&]() -> PyObject* { return PyBool_FromLong(needs_function(tensor_of(a[0], "x"), at::Tensor())); });
+    return layer_call([&]() -> PyObject* { return PyBool_FromLong(calls_are_seen() || has_tangent(tensor_of(a[0], "x"))); });
 }
 
 // int8_quantize(x, axis, q or None, scale or None) -> (q, scale)
