@@ -203,16 +203,20 @@ struct Int8Problem {
 
 // The way of a finished tile out of a warp: 32 rows (lane = row) x 128 bytes of the result at a time, scaled, the bias added and rounded, in
 // shared memory (16-byte piece j of row r at piece j ^ (r & 7), the swizzle of the tensor map: no two lanes meet in a bank), from where the
-// copy engine stores it and clips it at the matrix's edge. Stored by the lanes themselves, 32 bytes of 32 rows an instruction, the FP32 result
+// copy engine stores it. Stored by the lanes themselves, 32 bytes of 32 rows an instruction, the FP32 result
 // of 4096 x 4096 x 1024 took 30.6 us where the product without its stores takes 15.4. A result whose pitch or place is not a multiple of 16
 // bytes is copied out along its rows.
 constexpr int I8_BOX = 32 * 128;
+// The copy engine cuts a box off at the matrix's last row, but along the rows only at the next 16 bytes behind N: where N does not end on such a
+// border, boxes that go beyond it (`stop`) are copied out too.
 struct Int8Out {
     const CUtensorMap* map;      // null: no tensor map can be made
     void* y;
     int64_t ldy;
-    int M, N;
+    int M, N, stop;
 };
+template <class T>
+__device__ __forceinline__ int int8_stop(int N) { return N % (16 / (int)sizeof(T)) == 0 ? 0x7fffffff : N; }
 // Half of a box for 16-bit types, all of it for FP32: columns j0 .. j0 + 31 of it.
 template <class T>
 __device__ __forceinline__ void int8_fill_box(unsigned char* box, int j0, const int (&v)[32], float sa, const float* sb, const float* bias) {
@@ -237,7 +241,7 @@ __device__ __forceinline__ void int8_fill_box(unsigned char* box, int j0, const 
 template <class T, int COLS = 128 / (int)sizeof(T)>
 __device__ __forceinline__ void int8_send_box(const Int8Out& out, unsigned char* box, int row0, int col0) {
     const int lane = threadIdx.x & 31;
-    if (out.map) {
+    if (out.map && col0 + COLS <= out.stop) {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0 && row0 < out.M && col0 < out.N) {
@@ -363,7 +367,7 @@ int8_gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         if (mbar_wait_warp_soon(done_bar, 0, abort_flag, p.status, 175)) {
             tc_fence_after();
             constexpr int BOX = NT < 128 / (int)sizeof(T) ? NT : 128 / (int)sizeof(T);       // 32 columns of 16 bits fill half of a box: copied out
-            const Int8Out out{p.tma_out && BOX * sizeof(T) == 128 ? &mapY : nullptr, p.y, p.ldy, p.M, p.N};
+            const Int8Out out{p.tma_out && BOX * sizeof(T) == 128 ? &mapY : nullptr, p.y, p.ldy, p.M, p.N, int8_stop<T>(p.N)};
             unsigned char* box = boxes + (warp - 2) * I8_BOX;
 #pragma unroll
             for (int c = 0; c < NT; c += 32) {
@@ -504,7 +508,7 @@ int8_pair_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         float* sb = scales + e * 2 * C::COLS;
         unsigned char* box = sm + C::STAGES * C::STAGE + e * I8_BOX;
         const uint32_t tempty_leader = map_to_rank(tempty_bar, 0);
-        const Int8Out out{p.tma_out ? &mapY : nullptr, p.y, p.ldy, p.M, p.N};
+        const Int8Out out{p.tma_out ? &mapY : nullptr, p.y, p.ldy, p.M, p.N, int8_stop<T>(p.N)};
         constexpr int BOX = 128 / sizeof(T);
         uint32_t g = 0, gph = 0;
         for (int w = cluster; w < total; w += nclusters) {

@@ -1029,3 +1029,29 @@ def test_sequences_of_more_tokens_than_positions_have_bits_are_left_out(hb):
     many = hb.kv4_attention(normal(g, 200, 1, 64), cache, table[:1], i32([(1 << 30) - 1]))
     assert hb.device_status_rc() == (hb.ERR_INDEX, 1002) and many.isfinite().all() and many.any()
     assert all(torch.equal(a, b) for a, b in zip(arrays, old))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N", [1, 2, 3, 7, 31, 33, 60, 61, 62, 63, 65, 97, 126, 127, 129, 250, 252, 253])
+@pytest.mark.parametrize("M,times", [(1, 1), (5, 1), (300, 1), (300, 90)])
+def test_int8_gemm_stores_nothing_behind_a_row(hb, dtype, N, M, times):
+    """Results of every last column in rows on 16-byte borders that go on: what lies behind the last column, to the next border and beyond, stays."""
+    g = gen(N + M)
+    N, K = N + 256 * (times - 1), 70
+    x, w = normal(g, M, K).to(dtype), hb.int8_quantize(normal(g, N, K))
+    full = torch.full((M + 1, -(-(N + 9) // 8) * 8), 42.0, dtype=dtype, device="cuda")
+    out = full[:M, :N]
+    hb.int8_gemm(x, w, out=out)
+    check_product(hb, x, w, None, out)
+    out.fill_(42.0)
+    assert (full == 42.0).all()
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 40, 201), (3, 40, 250), (5, 40, 201), (40, 40, 129), (200, 96, 257), (200, 96, 300), (2500, 1500, 333), (40, 100, 17), (300, 300, 1)])
+def test_int8_gemm_reads_nothing_behind_the_contraction(hb, M, N, K):
+    """Both operands converted before and anything behind their rows, up to 31 bytes: exact sums of the first K."""
+    g = gen(K)
+    pitch = (K + 15) // 16 * 16 + 16
+    a, b = (torch.randint(-127, 128, (r, pitch), dtype=torch.int8, device="cuda", generator=g) for r in (M, N))
+    y = hb.int8_gemm(hb.Int8Rows(a, torch.ones(M, device="cuda"), K), hb.Int8Rows(b, torch.ones(N, device="cuda"), K))
+    assert torch.equal(y.double(), a[:, :K].double() @ b[:, :K].double().t())      # below 2^24: whole numbers in FP32
