@@ -35,7 +35,10 @@ template <int D, int NP> struct KpCfg {
     static constexpr int SOFT_WARPS = 4 * QT, FILL_WARPS = 4, THREADS = 32 * (SOFT_WARPS + FILL_WARPS + 4);      // the last four: one issues the MMAs
     // registers by role, out of what the launch has (512 x 128 or 384 x 168)
     static constexpr int REGS_SOFT = QT == 2 ? 168 : 232, REGS_FILL = QT == 2 ? 96 : 120, REGS_MMA = 56;
-    static_assert(32 * (SOFT_WARPS * REGS_SOFT + FILL_WARPS * REGS_FILL + 4 * REGS_MMA) <= THREADS * (QT == 2 ? 128 : 168) - 512, "register split");
+    static constexpr int REGS_LAUNCH = QT == 2 ? 128 : 168;
+    static_assert(65536 / THREADS / 8 * 8 == REGS_LAUNCH, "registers of the launch");
+    static_assert(32 * (SOFT_WARPS * REGS_SOFT + FILL_WARPS * REGS_FILL + 4 * REGS_MMA) <= THREADS * REGS_LAUNCH - 512, "register split");
+    static_assert(REGS_SOFT >= REGS_LAUNCH && REGS_FILL <= REGS_LAUNCH && REGS_MMA <= REGS_LAUNCH, "setmaxnreg.dec takes no number above the launch's, .inc none below");
     static constexpr int OFF_K = QT * NP * TILE, OFF_V = OFF_K + STAGES * KTILE, OFF_BAR = OFF_V + STAGES * KTILE;
     static constexpr int SMEM = 1024 + OFF_BAR + 512;
     static_assert(SMEM <= 232448, "shared memory");
