@@ -1055,3 +1055,100 @@ def test_int8_gemm_reads_nothing_behind_the_contraction(hb, M, N, K):
     a, b = (torch.randint(-127, 128, (r, pitch), dtype=torch.int8, device="cuda", generator=g) for r in (M, N))
     y = hb.int8_gemm(hb.Int8Rows(a, torch.ones(M, device="cuda"), K), hb.Int8Rows(b, torch.ones(N, device="cuda"), K))
     assert torch.equal(y.double(), a[:, :K].double() @ b[:, :K].double().t())      # below 2^24: whole numbers in FP32
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,N,K", [(2500, 4999, 2003), (4096, 4096, 1100), (3801, 1279, 1500), (38301, 380, 1030),        # pairs of SMs, 256, 256, 128, 128 channels
+                                   (1111, 777, 3001), (100, 6500, 1500), (100, 13000, 900), (129, 6500, 900), (128, 12800, 1024)])      # a tile per CTA, 64, 64, 128 ...
+def test_int8_gemm_of_many_tiles_and_stages(hb, dtype, M, N, K):
+    """Contractions of more steps than a kernel has stages, more tiles than it has accumulators; results stored as tiles (rows on 16-byte borders)
+    and element by element (rows off them), with nothing around them touched."""
+    g = gen(M + N + K)
+    x = normal(g, M, K).mul_(torch.exp(normal(g, M, 1))).to(dtype)
+    w = hb.int8_quantize(normal(g, N, K) * torch.exp(normal(g, N, 1)))
+    bias = normal(g, N)
+    y = hb.int8_gemm(x, w, bias=bias)
+    if dtype == torch.float16 and y.isinf().any():
+        # Beyond 65520, half a step behind binary16's largest number, the rounded result is an infinity. What is rounded is the FP32 result, which a
+        # call for that type gives and which the bound holds for; the rest of y is its rounding.
+        exact = hb.int8_gemm(x, w, bias=bias, dtype=torch.float32)
+        check_product(hb, x, w, bias, exact)
+        assert torch.equal(y.isinf(), exact.abs() >= 65520) and torch.equal(y, exact.half())
+    else:
+        check_product(hb, x, w, bias, y)
+    pitch = -(-(N + 8) // 8) * 8
+    for width, first in ((pitch, 0), (pitch + 1, 3)):
+        full = torch.full((M + 2, width), 42.0, dtype=dtype, device="cuda")
+        out = full[1:M + 1, first:first + N]
+        hb.int8_gemm(x, w, bias=bias, out=out)
+        assert torch.equal(out, y)
+        out.fill_(42.0)
+        assert (full == 42.0).all()
+
+
+def split_bytes(hb, dtype, heads, group, D, page, width, sequences, n, window):
+    """What a call of so many tokens a sequence asks for as workspace: 0 where its launch is one."""
+    import ctypes
+    from tests.test_serving_cpu import batch, cache
+    got = ctypes.c_size_t()
+    b = batch(sequences=sequences, tokens=sequences * n, max_tokens=n, table_pages=width, table_ld=width)
+    rc = hb.lib().hbfp_kv4_attention_workspace(ctypes.byref(cache(heads=heads, dim=D, page=page)), ctypes.byref(b), DTYPES.index(dtype), group, window, ctypes.byref(got))
+    assert rc == hb.OK
+    return got.value
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("heads,group,n,window,lengths", [
+    (16, 1, 1, 2000, [9000, 4096, 1999, 100, 0] * 3),            # many tiles: eight rows a CTA in the join, few parts of a tile
+    (8, 4, 3, 4096, [9000, 4096, 4099, 100, 2] * 3),             # 12 rows
+    (8, 5, 4, 4096, [9000, 4200, 1999, 3, 64] * 3),              # 20 rows (256 wide: two tiles of rows)
+    (2, 8, 1, 13000, [20000, 13000, 13063, 0]),                  # few tiles of many parts: a row a CTA in the join
+    (1, 3, 4, 13000, [20000, 13001, 300, 4]),
+    (1, 7, 4, 16000, [30000]),
+    (1, 8, 1, 30000, [60000] + [100] * 59)])                     # one tile of many parts among many tiles
+def test_attention_window_over_keys_that_are_split(hb, dtype, D, heads, group, n, window, lengths):
+    """A launch that shares out the units of all sequences' windows, and its join: sequences shorter and longer than the window, units that start
+    at its rounded edge."""
+    page = 64
+    many = D == 256 and dtype == torch.bfloat16 and group * n > 16 and window < 8000      # these take the kernel of many rows, in one launch
+    assert (split_bytes(hb, dtype, heads, group, D, page, -(-max(lengths) // page), len(lengths), n, window) > 0) != many
+    q, cache, table, y = check_attention(hb, dtype, heads, group, D, page, lengths, [n] * len(lengths), window=window)
+    assert torch.equal(hb.kv4_attention(q, cache, table, i32(lengths), window=window), y)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 96, 128])
+@pytest.mark.parametrize("heads,group,n,lengths", [(2, 3, 4, [20000, 700, 4]), (1, 16, 1, [40000]), (8, 4, 3, [9000, 5000, 3, 100] * 4), (4, 7, 4, [9000, 2049, 31, 640] * 6),
+                                                   (1, 4, 7, [70000] + [90] * 59)])
+def test_attention_wider_tiles_over_keys_that_are_split(hb, dtype, D, heads, group, n, lengths):
+    """Tiles of 16 and 32 rows in both forms of the join, with few and many parts."""
+    assert split_bytes(hb, dtype, heads, group, D, 64, -(-max(lengths) // 64), len(lengths), n, 0) > 0
+    check_attention(hb, dtype, heads, group, D, 64, lengths, [n] * len(lengths))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads,D,page", [(1, 64, 16), (3, 96, 32), (8, 128, 64), (2, 256, 16)])
+@pytest.mark.parametrize("count", [1, 5, 33, 71])
+def test_read_gives_what_was_written_and_zeros_where_there_is_no_position(hb, dtype, heads, D, page, count):
+    """Keys and values exactly, of more positions than some of the sequences have; the oracle's conversion is what was written."""
+    g = gen(D + count)
+    lengths = [0, 1, 2, 31, 32, 70, 131]
+    table, pages = pages_of(lengths, page, g)
+    cache = hb.kv4_alloc(pages, heads, page, D)
+    for t in (cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps):
+        t.fill_(0x5A)
+    x = (normal(g, sum(lengths), 2, heads, D) * torch.exp(2 * normal(g, 1, 2, heads, 1))).to(dtype)
+    starts = np.cumsum([0] + lengths)
+    hb.kv4_append(cache, x[:, 0], x[:, 1], table, i32(lengths), starts=i32(starts.tolist()))
+    got = hb.kv4_read(cache, count, table, i32(lengths))
+    for side in range(2):
+        q, s = oracle.quantize(np.ascontiguousarray(x[:, side].float().cpu().numpy().reshape(-1, D)), 1, oracle.Format(mant_bits=4, block=32))
+        value = (q.reshape(-1, D // 32, 32) * np.exp2(s.astype(np.float64))[..., None]).reshape(-1, heads, D)
+        want = np.zeros((len(lengths), count, heads, D))
+        for b, L in enumerate(lengths):
+            m = min(L, count)
+            if m:
+                want[b, count - m:] = value[starts[b + 1] - m:starts[b + 1]]
+        assert got[side].shape == (len(lengths) * count, heads, D) and got[side].dtype == torch.float32
+        assert np.array_equal(got[side].double().cpu().numpy(), want.reshape(-1, heads, D))
