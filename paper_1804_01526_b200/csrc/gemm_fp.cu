@@ -66,7 +66,7 @@ struct FpProblem {
     int M, N, nkb;
     int tiles_m, tiles_n;
     int splits, kb_per_split;     // splits > 1: the CTAs of a cluster share a tile
-    int tma_out;                  // C leaves through TMA stores (16-byte aligned, pitch of whole quads)
+    int tma_out;                  // C leaves through TMA stores (16-byte aligned, pitch and columns of whole quads)
     const float* bias;            // may be null
     float* C;
     int64_t ldc;
@@ -704,7 +704,8 @@ int fp_launch(FpProblem p, const FpOperand& a, const FpOperand& b, cudaStream_t 
         rc = make_map_f32(&mSB, b.scales, b.rs, p.nkb, b.rs, C::NOUT, C::BPS, false);
         if (rc) return rc;
     }
-    p.tma_out = FORM == FORM_S && p.splits == 1 && (reinterpret_cast<uintptr_t>(p.C) & 15) == 0 && (p.ldc & 3) == 0;
+    // (the copy engine cuts a box off at the next 16 bytes behind N, so N ends on such a border too)
+    p.tma_out = FORM == FORM_S && p.splits == 1 && (reinterpret_cast<uintptr_t>(p.C) & 15) == 0 && (p.ldc & 3) == 0 && (p.N & 3) == 0;
     if (p.tma_out) {
         rc = make_map_f32(&mC, p.C, p.N, p.M, p.ldc, 32, 32, true);
         if (rc) return rc;

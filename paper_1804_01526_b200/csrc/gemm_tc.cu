@@ -662,7 +662,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap mapA0, const __grid_constant_
                 // Each lane writes its row's 32 columns into a 128B-swizzled box (16-byte piece j of row r at
                 // piece j ^ (r & 7): conflict-free), one lane hands the box to the copy engine, and the warp goes
                 // on; a box is reused once the copy engine has read the one sent two boxes earlier. The copy
-                // clips what lies beyond M or N.
+                // clips what lies beyond M or N (along a row at 16-byte borders only, so N is a multiple of four).
 #pragma unroll
                 for (int cb = 0; cb < COLS_PER_WARP / 32; ++cb) {
                     const uint32_t buf = base + out_off + (uint32_t)((rwarp * 2 + (out_turn & 1)) * C::OUT_BUF);
@@ -893,7 +893,7 @@ int launch_gemm_tensor(int64_t M, int64_t N, int64_t K, const Packed& a, const P
     const bool magic = a.L.planes == 1 ? qa * qb * a.L.b < (1ll << 22) : 128ll * 128ll * a.L.b < (1ll << 22);
     // Short contractions are bound by the write of C: the tile then leaves through shared memory and TMA stores,
     // which the copy engine writes as whole lines while the warps go on with the next tile.
-    const bool tstore = p.splits == 1 && !P && a.L.nkb * a.L.bp <= 1024 && (reinterpret_cast<uintptr_t>(Cout) & 15) == 0 && (ldc % 4) == 0;
+    const bool tstore = p.splits == 1 && !P && a.L.nkb * a.L.bp <= 1024 && (reinterpret_cast<uintptr_t>(Cout) & 15) == 0 && (ldc % 4) == 0 && N % 4 == 0;
     if (P) {   // the inspection build of the kernel: 64-column tiles, writes the block sums
         p.tiles_n = (int)((N + 63) / 64);
         if (a.L.planes == 2) rc = magic ? launch_cfg<64, 2, true, true>(p, a, b, st) : launch_cfg<64, 2, false, true>(p, a, b, st);

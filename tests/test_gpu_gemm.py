@@ -829,3 +829,25 @@ def test_products_of_operands_that_the_kernel_before_has_written(hb, m, b, N, ki
         got.append(C.clone())
     assert all(torch.equal(x, y) for x, y in zip(got, want))
     assert hb.device_status() == 0
+
+
+@pytest.mark.parametrize("b", [16, 24, 32, 48, 64, 128, 512])
+@pytest.mark.parametrize("mant_bits", [8, 12])
+@pytest.mark.parametrize("M,N,K", [(700, 1021, 512), (2500, 2302, 768), (300, 511, 1024), (128, 129, 200), (4100, 4099, 640)])
+def test_nothing_is_stored_behind_a_row(hb, b, mant_bits, M, N, K):
+    """Results whose rows start on 16-byte borders and end off them, in a wider matrix: bit-equal to a result by itself, what lies behind stays."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(N + b)
+    A, B = torch.randn(M, K, device="cuda", generator=g), torch.randn(K, N, device="cuda", generator=g)
+    fmt = hb.Format(mant_bits, b)
+    want = hb.gemm(0, 0, A, B, fmt, fmt)
+    full = torch.full((M + 1, (N + 11) // 4 * 4), 42.0, device="cuda")
+    out = full[:M, :N]
+    hb.gemm(0, 0, A, B, fmt, fmt, out=out)
+    assert torch.equal(out, want)
+    out.fill_(42.0)
+    assert (full == 42.0).all()
+    w = hb.quantize(B, 0, fmt)
+    hb.gemm_q(M, N, K, A, w, fmtA=fmt, out=out)
+    out.fill_(42.0)
+    assert (full == 42.0).all()
