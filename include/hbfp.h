@@ -409,7 +409,8 @@ HBFP_API int hbfp_int8_quantize(const void* x, int dtype, int64_t d0, int64_t d1
  * or with a_dtype = HBFP_I8 rows that were converted before and their a_scale [M]; lda in elements
  * (HBFP_I8: bytes, a multiple of 16, a 16-byte aligned). w [N][ldw] with w_scale [N]: rows per output
  * channel, ldw a multiple of 16, w 16-byte aligned. bias: FP32 [N] or null. y of type y_dtype (not
- * HBFP_I8), ldy in elements. The workspace (256-byte aligned, hbfp_int8_gemm_workspace bytes, host-only
+ * HBFP_I8), ldy in elements. Where no workspace is asked for, y must not overlap a, which CTAs then read while
+ * others store (refused where the rows of both are equally far apart or there is one). The workspace (256-byte aligned, hbfp_int8_gemm_workspace bytes, host-only
  * query) holds converted activations where the product's kernel does not convert them itself. */
 HBFP_API int hbfp_int8_gemm_workspace(int64_t M, int64_t N, int64_t K, int a_dtype, size_t* bytes);
 HBFP_API int hbfp_int8_gemm(int64_t M, int64_t N, int64_t K, const void* a, int a_dtype, int64_t lda, const float* a_scale,
@@ -468,8 +469,8 @@ HBFP_API int hbfp_kv4_read(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* ba
 
 /* out[row][head] = sum_j p_j v_j with p = softmax_j(scale * q[row][head] . k_j) over the positions j <= own position
  * (and > own position - window where window > 0) of the row's sequence. q and out [tokens][heads*group][dim] (element strides,
- * dim contiguous); query head i reads KV head i / group. scale * log2(e) must be finite in FP32. A row that sees no key is zeros. Append the
- * call's own keys first. The workspace (256-byte aligned) takes the parts of a sequence that several CTAs share. */
+ * dim contiguous); query head i reads KV head i / group. scale * log2(e) must be finite in FP32. A row that sees no key is zeros. out may be
+ * q, or must not overlap it. Append the call's own keys first. The workspace (256-byte aligned) takes the parts of a sequence that several CTAs share. */
 HBFP_API int hbfp_kv4_attention_workspace(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int dtype, int32_t group,
                                           int32_t window, size_t* bytes);
 HBFP_API int hbfp_kv4_attention(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int dtype, const void* q, int64_t q_token,

@@ -510,7 +510,7 @@ def int8_gemm(x, w: Int8Rows, bias: Optional[torch.Tensor] = None, out: Optional
               dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """hbfp_int8_gemm: ``x [M][K]`` (a tensor, converted token by token by the call, or ``Int8Rows``) times the output channels
     ``w`` (rows = outputs), plus ``bias`` (float32 ``[N]``). The result ``[M][N]`` has x's type unless ``dtype`` or ``out`` says
-    otherwise (float32 for ``Int8Rows``)."""
+    otherwise (float32 for ``Int8Rows``). ``out`` may lie over a tensor x of more than three tokens, which is converted first; over others it is refused."""
     if isinstance(x, Int8Rows):
         if x.k != w.k:
             raise ValueError("contraction extents differ")
@@ -569,7 +569,7 @@ def kv4_attention(q: torch.Tensor, cache: Kv4Cache, page_table: torch.Tensor, le
     """hbfp_kv4_attention: causal attention of ``q [tokens][heads * group][dim]`` (any strides of tokens and heads) over the cache,
     the last ``window`` positions of it where that is not 0; ``scale`` (finite) is 1 / sqrt(dim) unless given. Tokens, ``page_table``, ``lengths``, ``starts`` and
     ``max_tokens`` as in ``kv4_append``, which writes the call's own keys and values first. A row that sees no key is zeros; rows behind the last sequence's are
-    left as they are (not set in a new result)."""
+    left as they are (not set in a new result). ``out`` may be q."""
     return _got((_native or host()).kv4_attention(cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps, page_table, lengths, q, scale, window, starts,
                                                   max_tokens, out), "hbfp_kv4_attention")
 

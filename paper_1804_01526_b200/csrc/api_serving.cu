@@ -24,6 +24,16 @@ constexpr int64_t MOST = 1ll << 30;                  // extents the kernels inde
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+// Whether two matrices of `rows` rows surely share bytes: their ranges meet and, with more than one row, their rows, equally far apart, do.
+bool share_bytes(const void* a, int64_t a_row, int64_t a_pitch, const void* b, int64_t b_row, int64_t b_pitch, int64_t rows) {
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
+    if (pa + ((rows - 1) * a_pitch + a_row) <= pb || pb + ((rows - 1) * b_pitch + b_row) <= pa) return false;
+    if (rows == 1) return true;
+    if (a_pitch != b_pitch) return false;
+    const int64_t d = pb >= pa ? (int64_t)((pb - pa) % a_pitch) : (a_pitch - (int64_t)((pa - pb) % a_pitch)) % a_pitch;      // columns from a's to b's
+    return d < a_row || d + b_row > a_pitch;
+}
+
 int kv4_args(const hbfp_kv4_cache* c, const hbfp_kv4_batch* b, Kv4Args* a) {
     if (!c || !b || c->struct_size != sizeof(*c) || b->struct_size != sizeof(*b)) return HBFP_ERR_INVALID_ARG;
     if (c->heads < 1 || c->pages < 0 || b->sequences < 0 || b->tokens < 0 || b->max_tokens < 0 || b->table_pages < 0 || b->table_ld < b->table_pages)
@@ -116,6 +126,9 @@ int hbfp_int8_gemm(int64_t M, int64_t N, int64_t K, const void* a, int a_dtype, 
             if (!a_scale) return HBFP_ERR_INVALID_ARG;
             if (lda % 16 != 0 || !aligned(a, 16)) return HBFP_ERR_ALIGNMENT;
         }
+        const int64_t a_bytes = a_dtype == HBFP_I8 ? 1 : dtype_bytes(a_dtype), y_bytes = dtype_bytes(y_dtype);
+        // (activations that are converted first have been read when the product stores)
+        if (need == 0 && share_bytes(a, K * a_bytes, lda * a_bytes, y, N * y_bytes, ldy * y_bytes, M)) return HBFP_ERR_INVALID_ARG;
         if (int8_few_eligible(M, K)) return launch_int8_few(M, N, K, a, a_dtype, lda, a_scale, w, ldw, w_scale, bias, y, y_dtype, ldy, st);
         if (a_dtype != HBFP_I8) {
             if (!workspace || workspace_bytes < need) return HBFP_ERR_WORKSPACE;

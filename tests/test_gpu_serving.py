@@ -1152,3 +1152,38 @@ def test_read_gives_what_was_written_and_zeros_where_there_is_no_position(hb, dt
                 want[b, count - m:] = value[starts[b + 1] - m:starts[b + 1]]
         assert got[side].shape == (len(lengths) * count, heads, D) and got[side].dtype == torch.float32
         assert np.array_equal(got[side].double().cpu().numpy(), want.reshape(-1, heads, D))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M", [1, 3, 16, 300])
+def test_int8_gemm_into_its_activations(hb, dtype, M):
+    """Refused where the product reads them itself (up to three tokens), right where they are converted first and in the other half of their rows."""
+    g = gen(71)
+    w = hb.int8_quantize(normal(g, 64, 64))
+    both = normal(g, M, 128).to(dtype)
+    x, y = both[:, :64], both[:, 64:]
+    want = hb.int8_gemm(x.clone(), w)
+    hb.int8_gemm(x, w, out=y)
+    assert torch.equal(y, want)
+    for out in (x, both[:, 32:96]):
+        if M > 3:
+            keep = x.clone()
+            assert torch.equal(hb.int8_gemm(x, w, out=out), want)
+            x.copy_(keep)
+            continue
+        with pytest.raises(hb.HbfpError) as e:
+            hb.int8_gemm(x, w, out=out)
+        assert e.value.code == hb.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("lengths,n,heads,group", [([40, 700], 1, 2, 4), ([5000, 3], 1, 4, 4), ([5000, 3, 1999] * 8, 1, 8, 2), ([20000, 40], 3, 2, 5), ([300, 600], 130, 2, 2), ([9000, 300], 130, 1, 2)])
+def test_attention_into_its_queries(hb, dtype, lengths, n, heads, group):
+    """Every row is read where it is written and before: one launch, clusters, split keys, many rows."""
+    g = gen(72)
+    table, pages = pages_of(lengths, 64, g)
+    cache = fill(hb, g, pages, heads, 64, 128)
+    q = normal(g, len(lengths) * n, heads * group, 128).to(dtype)
+    want = hb.kv4_attention(q, cache, table, i32(lengths))
+    assert hb.kv4_attention(q, cache, table, i32(lengths), out=q) is q
+    assert torch.equal(q, want)

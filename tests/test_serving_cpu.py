@@ -154,3 +154,26 @@ def test_attention_refuses_a_scale_that_is_no_number(hb):
         assert go(scale) == hb.ERR_INVALID_ARG, scale
     for scale in (0.0, -2.0, 1e-45, 2.3e38):
         assert go(scale) == hb.OK, scale
+
+
+def test_int8_gemm_refuses_a_result_over_activations_that_it_reads_itself(hb):
+    """Where the addresses say so. The other half of the same rows is another matrix; what is converted first has been read when results are stored.
+    (Calls that the check lets through are made only where there is no GPU for them to run on.)"""
+    f = hb.lib().hbfp_int8_gemm
+    A = 1 << 20
+
+    def call(y, M=3, N=20, K=20, ta=0, ty=0, lda=64, ldy=64):
+        return f(M, N, K, A, ta, lda, P if ta == 3 else None, P, 32, P, None, y, ty, ldy, None, 0, None)
+
+    for y in (A, A + 4 * 19, A + 4 * 45, A + 256, A - 4 * 19, A - 4 * 64, A + 4 * (128 + 19), A - 4 * (128 + 19)):
+        assert call(y) == hb.ERR_INVALID_ARG, y - A
+    assert call(A + 2 * 19, ta=1, ty=1) == hb.ERR_INVALID_ARG
+    assert call(A, M=1) == call(A + 4 * 19, M=1) == call(A - 4 * 19, M=1) == call(A + 4 * 19, M=1, ldy=32) == hb.ERR_INVALID_ARG
+    for M in (2, 7, 300):
+        assert call(A + 16, M=M, ta=3, lda=256, ldy=64) == hb.ERR_INVALID_ARG
+    assert call(A, M=7) == call(A, M=300) == hb.ERR_WORKSPACE
+    if torch.cuda.is_available():
+        return
+    for y in (A + 4 * 20, A + 4 * 44, A - 4 * 20, A - 4 * 44, A + 4 * (128 + 20), A + 4 * 192, A - 4 * 192, A - 4 * (128 + 20), A + (1 << 40)):
+        assert call(y) != hb.ERR_INVALID_ARG, y - A
+    assert call(A + 2 * 20, ta=1, ty=1) != hb.ERR_INVALID_ARG and call(A + 4 * 20, M=1, ldy=32) != hb.ERR_INVALID_ARG
