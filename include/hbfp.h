@@ -386,7 +386,8 @@ HBFP_API int hbfp_gemm_block_partials(int64_t M, int64_t N, int64_t K, const hbf
  * What a trained network is served with beside hbfp_gemm_q: a product in 8-bit integers with a
  * scale for each token and channel, and attention over a key/value cache held in 4-bit block
  * floating point. Activations are FP32, bfloat16 or binary16, sums are int32 or FP32, the result
- * has the activations' type. (The paper has no counterpart of the first; the cache is Eq. 1 with
+ * has the activations' type; attention weighs values with probabilities of 8, 16 or 24 bits for bfloat16, binary16 or
+ * FP32 queries (hbfp_kv4_attention). (The paper has no counterpart of the first; the cache is Eq. 1 with
  * 4-bit mantissas, the narrowest of its design points, blocks of 32.) */
 #define HBFP_F32 0
 #define HBFP_BF16 1
@@ -469,7 +470,9 @@ HBFP_API int hbfp_kv4_read(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* ba
 
 /* out[row][head] = sum_j p_j v_j with p = softmax_j(scale * q[row][head] . k_j) over the positions j <= own position
  * (and > own position - window where window > 0) of the row's sequence. q and out [tokens][heads*group][dim] (element strides,
- * dim contiguous); query head i reads KV head i / group. scale * log2(e) must be finite in FP32. A row that sees no key is zeros. out may be
+ * dim contiguous); query head i reads KV head i / group. scale * log2(e) must be finite in FP32. A row that sees no key is zeros. Scores, their
+ * maximum and sum, and the sum over the values are FP32; a probability is rounded once more where it meets its value, to 1, 2 or 3 bfloat16 parts
+ * (2^-8, 2^-16, 2^-24) for queries of bfloat16, binary16 or FP32. At most 65535 sequences and query heads. out may be
  * q, or must not overlap it. Append the call's own keys first. The workspace (256-byte aligned) takes the parts of a sequence that several CTAs share. */
 HBFP_API int hbfp_kv4_attention_workspace(const hbfp_kv4_cache* cache, const hbfp_kv4_batch* batch, int dtype, int32_t group,
                                           int32_t window, size_t* bytes);

@@ -539,7 +539,7 @@ class Kv4Cache:
 
 def kv4_alloc(pages: int, heads: int, page: int, dim: int, device="cuda") -> Kv4Cache:
     """An empty cache: ``pages`` pages of ``page`` tokens (a power of two, 16 or more) of ``heads`` KV heads of ``dim`` values
-    (64, 96, 128 or 256). Nothing reads a row that was not appended, so it is not cleared."""
+    (64, 96, 128 or 256). Rows that were not appended may be loaded with others of their page, but no result depends on them, so it is not cleared."""
     if page < 16 or page & (page - 1) or dim not in (64, 96, 128, 256) or pages < 0 or heads < 1:
         raise ValueError("page must be a power of two, 16 or more, dim one of 64, 96, 128 and 256")
     m = [torch.empty((pages, heads, page, dim // 2), dtype=torch.uint8, device=device) for _ in range(2)]
@@ -569,7 +569,10 @@ def kv4_attention(q: torch.Tensor, cache: Kv4Cache, page_table: torch.Tensor, le
     """hbfp_kv4_attention: causal attention of ``q [tokens][heads * group][dim]`` (any strides of tokens and heads) over the cache,
     the last ``window`` positions of it where that is not 0; ``scale`` (finite) is 1 / sqrt(dim) unless given. Tokens, ``page_table``, ``lengths``, ``starts`` and
     ``max_tokens`` as in ``kv4_append``, which writes the call's own keys and values first. A row that sees no key is zeros; rows behind the last sequence's are
-    left as they are (not set in a new result). ``out`` may be q."""
+    left as they are (not set in a new result). ``out`` may be q.
+
+    Which kernel runs goes by the most tokens of a sequence and by the table's width, which the host knows: prompts beside many single tokens, and
+    short sequences in a table for long ones, take less time in a call of their own and with ``page_table[:, :pages]``."""
     return _got((_native or host()).kv4_attention(cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps, page_table, lengths, q, scale, window, starts,
                                                   max_tokens, out), "hbfp_kv4_attention")
 

@@ -27,7 +27,7 @@ int8_rows_kernel(const T* __restrict__ x, int64_t rows, int64_t k, int64_t ld, b
     if (GROUP <= 32 && row >= rows) return;                          // (whole warps; with larger groups they stay for the barrier)
     const bool in = row < rows;
     const T* src = x + (in ? row : 0) * ld;
-    const int pieces = in ? (int)(pitch / 8) : 0, whole = (int)(k / 8);      // of eight values; the row ends inside one of the last two
+    const int pieces = in ? (int)(pitch / 8) : 0, whole = (int)(k / 8);      // of eight values; those behind k are zeros, as many as the pitch has
     Eight<T> v[QR_KEEP];
     const T* const end = x + (rows - 1) * ld + k;
     auto fetch = [&](int i, Eight<T>& e) {
@@ -160,7 +160,7 @@ int8_shifted_rows_kernel(const T* __restrict__ x, int64_t rows, int64_t k, int64
 }
 
 // Columns of x [k][cols] to q [cols][pitch] and scale [cols]: weights stored with the contraction down their rows, converted once.
-// 32 columns per CTA: the largest values first, then tiles of 128 rows turned in shared memory.
+// 32 columns per CTA: the largest values first, then tiles of 128 rows turned in shared memory. Reads twice, with few CTAs: 4096 x 4096 FP32 139 us.
 template <class T>
 __global__ void __launch_bounds__(256)
 int8_columns_kernel(const T* __restrict__ x, int64_t k, int64_t cols, int64_t ld, int8_t* __restrict__ q, int64_t pitch, float* __restrict__ scale) {

@@ -4,8 +4,9 @@
 // around it. A CTA takes 16 channels at a time and all of K, an eighth of it per warp: a lane loads 16 bytes of two channels at a time straight into
 // MMA operand registers (the order of the values along an MMA's contraction is free as long as both operands agree), the first of them before
 // anything else is known. The tokens lie in shared memory as bytes; every CTA converts them itself, which saves a launch. Sums of the warps are
-// int32 and add up exactly. One token, 4096 x 4096: 7.3 us (two launches, tiles of 128 x 128: 13.0; conversion and tcgen05 MMAs in one launch, K
-// split over a cluster: 12.9, most of it waits for the other CTAs). Two 8.4 and three 9.8; four 10.8 where a conversion and int8_gemm_kernel take 9.1.
+// int32 and add up exactly. One token, 4096 x 4096, bfloat16: 5.6 us among others (cold 9.5), two 6.9, three 8.0; four
+// took 10.8 when tried, where a conversion and int8_gemm_kernel take 8.5 to 9.2. (Tried for one token, when this kernel took 7.3: two launches with tiles of
+// 128 x 128 13.0; conversion and tcgen05 MMAs in one launch, K split over a cluster, 12.9, most of it waits for the other CTAs.)
 #include "int8.cuh"
 
 namespace hbfp {

@@ -7,7 +7,7 @@
 // contraction is free as long as both operands agree, so the unpacked pairs need no shuffling; scores become the second product's
 // operand by one 8 x 8 transpose (movmatrix).
 //
-// A cached value, nibble * 2^s, is a bfloat16 exactly: (128 + nibble) is put together with one logical instruction and
+// A cached value, nibble * 2^s, is a bfloat16 exactly: (128 + nibble) is put together with one logical instruction (a published technique) and
 // fma(128 + nibble, 2^s, -136 * 2^s) rounds nothing. Queries and probabilities are split into as many bfloat16 parts as their type
 // has bits (1 for bfloat16, 2 for binary16, 3 for FP32: of a query nothing is left, of a probability 2^-8, 2^-16, 2^-24), so
 // products are exact and sums FP32. Softmax in base 2, running maximum and sum in FP32.

@@ -9,7 +9,7 @@
 // tiles do not fill the GPU, the CTAs of a cluster share a tile's keys and join their results through shared memory.
 //
 // Queries and probabilities have as many bfloat16 parts as their type has bits (1, 2 or 3 as in kv4_attend.cuh), each an MMA of its own.
-// The maximum is only moved, and O rescaled, when a row's scores exceed it by more than 2^8: probabilities up to 2^8 lose nothing in FP32 and
+// The maximum is only moved, and O rescaled, when a row's scores exceed it by more than 2^8 (a published technique): probabilities up to 2^8 lose nothing in FP32 and
 // bfloat16, and the sum is divided out with the same maximum.
 //
 // Bound: per 128 keys and 256 rows 2048 cycles of MMA (bfloat16, 128 wide) and as many of exponentials.
@@ -669,7 +669,7 @@ int kp_launch_dim(const Kv4Attend& a, cudaStream_t st) {
 // More rows than the widest tile of the kernel of few rows (32, of a 256-wide head 16), which reads the keys once for each such tile but spreads any
 // number of tiles over all SMs, where a row tile here is no more than a cluster's. An SM's time for a key, of such a tile there and of a CTA's rows
 // here, in ns: 128 wide 13 / 18 (bfloat16), 19 / 24 (binary16), 24 / 37 (FP32); 96 wide 13 / 19, 18 / 24, 23 / 34; 256 wide 18 / 30, 23 / 61. Up to 8192
-// keys it is the launches that count, one here. Measured, 8 heads, bfloat16, few / here: 40 rows of 128 in 32 sequences with 4096 keys 179 / 145 us, in one
+// keys (1024 where the ratio is above two, 256 wide binary16) it is the launches that count, one here. Measured, 8 heads, bfloat16, few / here: 40 rows of 128 in 32 sequences with 4096 keys 179 / 145 us, in one
 // with 4096 20.5 / 16.5, with 32768 53 / 76; 96 rows 273 / 145, 21.6 / 17.7, 74 / 77. 512 rows of 32 sequences with 2048 keys, 96 wide 641 / 167, 256 wide
 // 1813 / 422. FP32 queries of 256 have no room in shared memory.
 bool kv4_prompt_eligible(const Kv4Attend& a, int dtype) {
