@@ -443,7 +443,7 @@ typedef struct hbfp_kv4_cache {
  * not written to the cache and sees no key. Rows behind the last sequence's are left as they are. A length
  * of 0 or less is an empty sequence. Where a length goes beyond the page table, the positions that the table
  * has no page for are not written, not seen and read as zeros, and all others are what they would be; a
- * sequence of 2^30 or more is left out, as is one with more than max_tokens rows or starts out of order.
+ * sequence of 2^30 or more is left out (reads as zeros), as is one with more than max_tokens rows or starts out of order.
  * hbfp_device_status then reports it. Set struct_size. */
 typedef struct hbfp_kv4_batch {
     uint32_t struct_size;

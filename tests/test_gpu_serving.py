@@ -1187,3 +1187,18 @@ def test_attention_into_its_queries(hb, dtype, lengths, n, heads, group):
     want = hb.kv4_attention(q, cache, table, i32(lengths))
     assert hb.kv4_attention(q, cache, table, i32(lengths), out=q) is q
     assert torch.equal(q, want)
+
+
+def test_a_sequence_that_is_left_out_reads_as_zeros(hb):
+    """Not as whatever the new result's memory held."""
+    g = gen(81)
+    cache = fill(hb, g, 3, 2, 16, 64)
+    table = i32([[0, 1, 2]] * 3)
+    want = hb.kv4_read(cache, 7, table[:1], i32([40]))
+    for _ in range(3):
+        junk = [torch.full((3 * 7, 2, 64), 5.0, device="cuda") for _ in range(8)]
+        del junk
+        k, v = hb.kv4_read(cache, 7, table, i32([1 << 30, 40, 2 ** 31 - 1]))
+        assert hb.device_status_rc() == (hb.ERR_INDEX, 1002)
+        assert not k[:7].any() and not v[:7].any() and not k[14:].any() and not v[14:].any()
+        assert torch.equal(k[7:14], want[0]) and torch.equal(v[7:14], want[1])
