@@ -442,9 +442,9 @@ typedef struct hbfp_kv4_cache {
  * each. Row i of n of a sequence stands at position length - n + i; a row whose position is negative is
  * not written to the cache and sees no key. Rows behind the last sequence's are left as they are. A length
  * of 0 or less is an empty sequence. Where a length goes beyond the page table, the positions that the table
- * has no page for are not written, not seen and read as zeros, and all others are what they would be; a
- * sequence of 2^30 or more is left out (reads as zeros), as is one with more than max_tokens rows or starts out of order.
- * hbfp_device_status then reports it. Set struct_size. */
+ * has no page for are not written, not seen and read as zeros, and all others are what they would be (a
+ * length of 2^30 or more counts as 0); a sequence with more than max_tokens rows or starts out of order is
+ * left out. hbfp_device_status then reports it. Set struct_size. */
 typedef struct hbfp_kv4_batch {
     uint32_t struct_size;
     int32_t sequences;

@@ -96,8 +96,7 @@ kv4_read_kernel(Kv4Args a, int count, float* __restrict__ k, float* __restrict__
     const int b = blockIdx.y;
     a.starts = nullptr;
     a.most = count;
-    Kv4Seq s = kv4_seq_unreported(a, b);
-    s.n = count;                          // (of a sequence that is left out all positions read as zeros)
+    const Kv4Seq s = kv4_seq_unreported(a, b);
     const W w(a.heads);
     if (w.idle()) return;
     for (int64_t t0 = (int64_t)blockIdx.x * w.tokens; t0 < s.n; t0 += (int64_t)gridDim.x * w.tokens * KV4_UNROLL)

@@ -61,8 +61,7 @@ __device__ __forceinline__ Kv4Seq kv4_seq_unreported(const Kv4Args& a, int b) {
     }
     const int cap = (int)((int64_t)a.table_pages << a.shift);             // (below 2^30)
     const int len = __ldg(a.lengths + b);
-    s.length = len < 0 ? 0 : len;
-    if (len >= 1 << 30) { s.length = 0; s.n = 0; }                        // positions have 30 bits: all of the sequence is left out
+    s.length = (uint32_t)len < 1u << 30 ? len : 0;                         // positions have 30 bits: a longer sequence counts as an empty one
     s.held = min(s.length, cap);
     s.bad = bad || len > cap;
     return s;

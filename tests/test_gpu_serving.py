@@ -1011,7 +1011,7 @@ def test_attention_behind_the_page_table(hb, dtype, D, pages, length, n, window)
         assert (y[:, h].double() - ref).abs().le(tol).all(), ((y[:, h].double() - ref).abs() / tol).max()
 
 
-def test_sequences_of_more_tokens_than_positions_have_bits_are_left_out(hb):
+def test_sequences_of_more_tokens_than_positions_have_bits_are_empty(hb):
     g = gen(61)
     cache = fill(hb, g, 3, 1, 16, 64)
     arrays = (cache.k_mant, cache.k_exps, cache.v_mant, cache.v_exps)
@@ -1023,9 +1023,9 @@ def test_sequences_of_more_tokens_than_positions_have_bits_are_left_out(hb):
         assert hb.device_status_rc() == (hb.ERR_INDEX, 1002)
         y = hb.kv4_attention(k, cache, table, i32([length, 40]), out=torch.full_like(k, 3.0))
         assert hb.device_status_rc() == (hb.ERR_INDEX, 1002)
-        assert (y[0] == 3.0).all() and torch.equal(y[1], good[1])
+        assert not y[0].any() and torch.equal(y[1], good[1])
         many = hb.kv4_attention(normal(g, 200, 1, 64), cache, table[:1], i32([length]), window=2 ** 31 - 1, out=torch.full((200, 1, 64), 3.0, device="cuda"))
-        assert hb.device_status_rc() == (hb.ERR_INDEX, 1002) and (many == 3.0).all()
+        assert hb.device_status_rc() == (hb.ERR_INDEX, 1002) and not many.any()
     many = hb.kv4_attention(normal(g, 200, 1, 64), cache, table[:1], i32([(1 << 30) - 1]))
     assert hb.device_status_rc() == (hb.ERR_INDEX, 1002) and many.isfinite().all() and many.any()
     assert all(torch.equal(a, b) for a, b in zip(arrays, old))
@@ -1189,7 +1189,7 @@ def test_attention_into_its_queries(hb, dtype, lengths, n, heads, group):
     assert torch.equal(q, want)
 
 
-def test_a_sequence_that_is_left_out_reads_as_zeros(hb):
+def test_a_sequence_too_long_for_positions_reads_as_zeros(hb):
     """Not as whatever the new result's memory held."""
     g = gen(81)
     cache = fill(hb, g, 3, 2, 16, 64)
