@@ -557,6 +557,8 @@ kv4_prompt_kernel(const Kv4Attend a, int splits) {
                 // rows an instruction took 2 us.
                 constexpr int V = 16 / sizeof(T), PIECES = D / V, LINE = (PIECES + 7) / 8 * 128, RPS = 32 / PIECES > 0 ? 32 / PIECES : 1;
                 unsigned char* area = sm + (t * 4 + quarter) * 32 * LINE;
+                // (a tile without a key has no MMAs to wait for, but its other warps may still be bringing queries)
+                if (mine == 0) asm volatile("bar.sync %0, 128;" ::"r"(2 + t) : "memory");
 #pragma unroll
                 for (int c = 0; c < D; c += 32) {
                     uint32_t v[32];

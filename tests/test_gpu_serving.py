@@ -1202,3 +1202,22 @@ def test_a_sequence_too_long_for_positions_reads_as_zeros(hb):
         assert hb.device_status_rc() == (hb.ERR_INDEX, 1002)
         assert not k[:7].any() and not v[:7].any() and not k[14:].any() and not v[14:].any()
         assert torch.equal(k[7:14], want[0]) and torch.equal(v[7:14], want[1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("heads,group,n,window", [(1, 3, 96, 0), (8, 4, 224, 0), (3, 1, 300, 5), (2, 7, 188, 0), (8, 8, 43, 30)])
+def test_attention_of_padded_batches_of_many_rows(hb, dtype, D, heads, group, n, window):
+    """Sequences far shorter than their rows: whole row tiles without a key are zeros, every time, whatever their queries and what the result held."""
+    lengths = [0, 1, n, 0, 7, n + 40, 1]
+    g = gen(D + n)
+    table, pages = pages_of(lengths, 32, g)
+    cache = fill(hb, g, pages, heads, 32, D)
+    q = normal(g, len(lengths) * n, heads * group, D).to(dtype)
+    ref, tol = attend_reference(q, cache, table, lengths, [n] * len(lengths), D ** -0.5, window)
+    out = torch.empty_like(q)
+    for _ in range(10):
+        hb.kv4_attention(q, cache, table, i32(lengths), window=window, out=out.fill_(9.0))
+        assert (out.double() - ref).abs().le(tol).all()
+        for b, L in enumerate(lengths):
+            assert not out[b * n:(b + 1) * n - L].any()
